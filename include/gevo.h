@@ -522,6 +522,190 @@ gevo_status gevo_cnn_kernel_stats(gevo_cnn* h, int kind, double* total_ms, uint6
 
 void gevo_cnn_destroy(gevo_cnn* h);
 
+/* ------------------------------------------------------------------------
+ * Operators on device arrays: rows routed to experts, and layers in 4 bits.
+ * A population's variants can serve together, every row going to the few of
+ * them that a router chooses for it: gevo_pop_layer_weights gives a layer of
+ * every variant as one array of weight matrices, the experts below.
+ *
+ * These calls hold no state and take no handle.  Every pointer named d_ is
+ * device memory of the caller's, on the current device, which has to be
+ * hip_stream's; work is enqueued on hip_stream and nothing synchronises, so
+ * calls may be captured into a graph (each call's workspace then belongs to
+ * that graph).  Calls that share no output or workspace may run at once on
+ * several streams.  Arguments are checked before any HIP call: GEVO_E_ARG for
+ * a null or misaligned pointer (of its element's size, 16 bytes for 4-bit
+ * codes and 4 for their scales) or a bad enum, GEVO_E_SHAPE for a size of 0
+ * or a stride below a row, GEVO_E_UNSUPPORTED beyond the limits.  No rows (T
+ * or S of 0) is allowed: outputs over rows are then left, sums are 0.  Strides
+ * count elements.  Results are the same bits on every run.
+ *
+ * Sums, softmax, scores and joins are held in fp32; an output in bf16 is
+ * rounded once, to nearest even.
+ * ------------------------------------------------------------------------ */
+#define GEVO_MAX_EXPERTS 2048u
+#define GEVO_MAX_TOP_K 64u
+#define GEVO_MAX_GROUPS 64u
+
+/* W_l of every variant as [P][d_l][d_{l-1}] (a unit's inputs contiguous) in
+ * dtype (bf16: rounded to nearest even from the fp32 master) and its biases
+ * [P][d_l]; layer 1 .. n_layers.  Either output may be NULL.  Asynchronous on
+ * the handle's stream. */
+gevo_status gevo_pop_layer_weights(gevo_pop* pop, uint32_t layer, gevo_dtype dtype, void* d_w, float* d_b);
+
+typedef enum { GEVO_SCORE_SOFTMAX = 0, GEVO_SCORE_SIGMOID = 1 } gevo_score;
+
+/*
+ * Choice of k of E experts for each of T rows of logits (dtype, rows
+ * logits_stride elements apart).  Scores s are the softmax over the row's E
+ * logits or each one's sigmoid.  The choice goes by keys: s + bias (d_bias,
+ * [E], a balance that does not enter the weights); without a bias and with
+ * group_top 1 the logits themselves, which order alike.  With groups > 1 the E
+ * keys form `groups` runs of E / groups; a group's value is the sum of its
+ * group_top (1 or 2) largest keys, and the experts of the top_groups groups
+ * with the largest values stay.  ids: the k largest keys among these,
+ * descending; equal keys and groups go to the lowest index.  Keys are compared
+ * as if scores had 64 bits.  weights: scale * s, with renorm scale * s / (sum
+ * of the chosen s).
+ *
+ * A logit (or bias) of -inf takes its expert out: it is never chosen and adds
+ * nothing to a group.  Slots that find no expert get id -1 and weight 0.  A
+ * row with a NaN logit or key, or with a logit of +inf under softmax, gets ids
+ * -1 and weights NaN.
+ */
+typedef struct {
+  uint32_t abi_version;
+  uint32_t E, k;               /* 1 .. GEVO_MAX_EXPERTS, 1 .. min(E, GEVO_MAX_TOP_K) */
+  int64_t T;                   /* rows; T * k below 2^31 */
+  gevo_dtype dtype;            /* of the logits (and of their gradient) */
+  gevo_score score;
+  int64_t logits_stride;       /* >= E */
+  uint32_t groups;             /* 1 .. GEVO_MAX_GROUPS, a divisor of E */
+  uint32_t top_groups;         /* 1 .. groups */
+  uint32_t group_top;          /* 1 or 2 */
+  uint32_t renorm;             /* 0 or 1 */
+  float scale;                 /* finite */
+} gevo_route_config;
+
+gevo_status gevo_route(const gevo_route_config* cfg, const void* d_logits, const float* d_bias, float* d_weights,
+                       int32_t* d_ids, void* hip_stream);
+
+/* Gradient of the weights with respect to the logits: d_dweights [T][k] fp32
+ * to d_dlogits [T][E] (contiguous, in dtype), with the choice d_ids held
+ * fixed.  groups, top_groups and group_top are not read.  An id outside [0, E)
+ * contributes nothing; an id that a row holds twice contributes both terms. */
+gevo_status gevo_route_backward(const gevo_route_config* cfg, const void* d_logits, const int32_t* d_ids,
+                                const float* d_dweights, void* d_dlogits, void* hip_stream);
+
+/*
+ * The slots of a routing (slot t k + j is choice j of row t; `slots` of them)
+ * sorted by expert, slots of one expert in their own order:
+ *   offsets[E + 1]  expert e's sorted rows are offsets[e] .. offsets[e + 1)
+ *   order[slots]    slot of each sorted row; entries from offsets[E] on are left
+ *   pos[slots]      sorted row of each slot, -1 where the id is outside [0, E)
+ * d_ws: gevo_route_plan_bytes bytes, 4-byte aligned.
+ */
+gevo_status gevo_route_plan_bytes(int64_t slots, uint32_t E, size_t* bytes);
+gevo_status gevo_route_plan(int64_t slots, uint32_t E, const int32_t* d_ids, void* d_ws, size_t ws_bytes,
+                            int32_t* d_order, int32_t* d_pos, int32_t* d_offsets, void* hip_stream);
+
+/*
+ * A layer of every expert on the rows it was chosen for.  Sorted row r of
+ * expert e reads row order[r] / k of x ([T][K]); with sorted_rows, x holds the
+ * sorted rows themselves ([S][K], S = T k; a further layer).
+ *   forward   out[r][n] = act(sum_k x[row(r)][k] w[e][n][k] + bias[e][n])
+ *             with act the identity or (relu) max(., 0); NaN stays NaN
+ *   backward  from dy[S][N], the gradient of the product before act:
+ *             dx[r][k] = sum_n dy[r][n] w[e][n][k], for each sorted row (with
+ *             relu_input 0 where x[row(r)][k] is not > 0: x is then the
+ *             output of a ReLU and dx the gradient before it),
+ *             dw[e][n][k] = sum_r dy[r][n] x[row(r)][k] and
+ *             db[e][n] = sum_r dy[r][n] over expert e's rows (0 without any).
+ * x, w, dy and dx have dtype; dw and db are fp32.  Sums are fp32.  A
+ * gradient's outputs may be NULL; dw, db and dx are contiguous.  Sorted rows
+ * from offsets[E] on are not written.  Offsets outside [0, S] are cut to it,
+ * and a row outside x reads zeros.
+ */
+typedef struct {
+  uint32_t abi_version;
+  gevo_dtype dtype, out_dtype;   /* out_dtype: of the forward output */
+  uint32_t E, k, N, K;           /* N, K up to 2^20 */
+  int64_t T;                     /* T * k below 2^31 */
+  int64_t x_stride;              /* rows of x, >= K */
+  int64_t w_stride_e, w_stride_n;/* matrices, >= (N - 1) w_stride_n + K; rows of one, >= K */
+  int64_t y_stride;              /* rows of the forward output or of dy, >= N */
+  uint32_t sorted_rows;
+  uint32_t relu;                 /* forward: relu; backward: relu_input */
+} gevo_expert_config;
+
+gevo_status gevo_expert_forward(const gevo_expert_config* cfg, const void* d_x, const void* d_w, const float* d_bias,
+                                const int32_t* d_order, const int32_t* d_offsets, void* d_out, void* hip_stream);
+gevo_status gevo_expert_backward(const gevo_expert_config* cfg, const void* d_dy, const void* d_x, const void* d_w,
+                                 const int32_t* d_order, const int32_t* d_offsets, void* d_dx, float* d_dw,
+                                 float* d_db, void* hip_stream);
+
+/*
+ * The join: y[t] = sum_j weights[t][j] rows[pos[t][j]], in j's order (weights
+ * NULL: ones); a slot without a row counts as a row of zeros.  The gradient:
+ * drows[pos[t][j]] = weights[t][j] dy[t] (contiguous [T k][N]) and
+ * dweights[t][j] = sum_n dy[t][n] rows[pos[t][j]][n] (0 without a row); either
+ * may be NULL, rows too where dweights is.  dy, rows and drows have dtype.
+ */
+typedef struct {
+  uint32_t abi_version;
+  gevo_dtype dtype, out_dtype;   /* of the rows; of y (forward) */
+  uint32_t k, N;
+  int64_t T;
+  int64_t rows_stride, y_stride; /* >= N */
+} gevo_combine_config;
+
+gevo_status gevo_expert_combine(const gevo_combine_config* cfg, const void* d_rows, const int32_t* d_pos,
+                                const float* d_weights, void* d_y, void* hip_stream);
+gevo_status gevo_expert_combine_backward(const gevo_combine_config* cfg, const void* d_dy, const void* d_rows,
+                                         const int32_t* d_pos, const float* d_weights, void* d_drows,
+                                         float* d_dweights, void* hip_stream);
+
+/*
+ * Microscaled 4-bit floating point (OCP Microscaling Formats v1.0: MXFP4).
+ * Along a row, 32 values share a scale 2^X, X = floor(log2 of the largest
+ * magnitude) - 2, not below -127; a value is held as the one of 0, 0.5, 1,
+ * 1.5, 2, 3, 4, 6 and their negatives nearest to v / 2^X, ties to the even
+ * index, magnitudes above 6 as 6.  A block with a NaN or an infinity reads as
+ * NaN throughout.  Layout of [rows][K], with Kp = K rounded up to 128:
+ *   codes  [rows][Kp / 2]   value 2 i in the low half of byte i; bit 3 the sign,
+ *                           bits 0 - 2 the index in the list above
+ *   scales [rows][Kp / 32]  X + 127; 255 for NaN
+ * Values past K are zero.
+ */
+gevo_status gevo_mx4_quantize(gevo_dtype dtype, int64_t rows, uint32_t K, const void* d_x, int64_t x_stride,
+                              uint8_t* d_codes, uint8_t* d_scales, void* hip_stream);
+/* The values: exact in fp32; in bf16 exact unless below its normal range. */
+gevo_status gevo_mx4_dequantize(gevo_dtype dtype, int64_t rows, uint32_t K, const uint8_t* d_codes,
+                                const uint8_t* d_scales, void* d_x, int64_t x_stride, void* hip_stream);
+
+/*
+ * Products of 4-bit rows a ([rows][K]) with P 4-bit matrices b ([P][N][K]),
+ * fp32 sums:
+ *   dense (d_offsets NULL): out[p][m][n] = act(sum_k a[m][k] b[p][n][k] +
+ *     bias[p][n]) for M rows, a shared by all p or (a_each) [P][M][K]
+ *   routed: as gevo_expert_forward over the sorted rows, E = P experts,
+ *     a [M][K] with M = T rows chosen k each, or (sorted_rows) [M k][K]
+ * out is contiguous, [P][M][N] or [M k][N], in out_dtype.
+ */
+typedef struct {
+  uint32_t abi_version;
+  gevo_dtype out_dtype;
+  uint32_t P, N, K;              /* N, K up to 2^20 */
+  int64_t M;                     /* P * M, and routed M * k, below 2^31 */
+  uint32_t a_each;
+  uint32_t k, sorted_rows;       /* routed */
+  uint32_t relu;
+} gevo_mx4_config;
+
+gevo_status gevo_mx4_matmul(const gevo_mx4_config* cfg, const uint8_t* d_a_codes, const uint8_t* d_a_scales,
+                            const uint8_t* d_b_codes, const uint8_t* d_b_scales, const float* d_bias,
+                            const int32_t* d_order, const int32_t* d_offsets, void* d_out, void* hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

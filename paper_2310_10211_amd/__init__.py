@@ -41,6 +41,9 @@ EXPORTED = [
     "gevo_genomes_breed", "gevo_pop_set_genomes", "gevo_pop_set_grad_scale",
     "gevo_cnn_param_count", "gevo_cnn_workspace_bytes", "gevo_cnn_init", "gevo_cnn_predict", "gevo_cnn_scores",
     "gevo_cnn_export", "gevo_cnn_remove_layer", "gevo_cnn_destroy", "gevo_cnn_set_profiling", "gevo_cnn_kernel_stats",
+    "gevo_pop_layer_weights", "gevo_route", "gevo_route_backward", "gevo_route_plan_bytes", "gevo_route_plan",
+    "gevo_expert_forward", "gevo_expert_backward", "gevo_expert_combine", "gevo_expert_combine_backward",
+    "gevo_mx4_quantize", "gevo_mx4_dequantize", "gevo_mx4_matmul",
 ]
 CNN_MAX_BLOCKS = 4
 CNN_KERNEL_KINDS = ["stem", "depthwise", "pointwise", "pool", "head", "reduce", "pw_dw"]
@@ -163,6 +166,18 @@ def lib():
         L.gevo_cnn_set_profiling.argtypes = [vp, ctypes.c_int]
         L.gevo_cnn_kernel_stats.argtypes = [vp, ctypes.c_int, ctypes.POINTER(ctypes.c_double),
                                             ctypes.POINTER(ctypes.c_uint64)]
+        L.gevo_pop_layer_weights.argtypes = [vp, u32, ctypes.c_int, vp, vp]
+        L.gevo_route.argtypes = [vp] * 6
+        L.gevo_route_backward.argtypes = [vp] * 6
+        L.gevo_route_plan_bytes.argtypes = [i64, u32, ctypes.POINTER(ctypes.c_size_t)]
+        L.gevo_route_plan.argtypes = [i64, u32, vp, vp, ctypes.c_size_t, vp, vp, vp, vp]
+        L.gevo_expert_forward.argtypes = [vp] * 8
+        L.gevo_expert_backward.argtypes = [vp] * 10
+        L.gevo_expert_combine.argtypes = [vp] * 6
+        L.gevo_expert_combine_backward.argtypes = [vp] * 8
+        L.gevo_mx4_quantize.argtypes = [ctypes.c_int, i64, u32, vp, i64, vp, vp, vp]
+        L.gevo_mx4_dequantize.argtypes = [ctypes.c_int, i64, u32, vp, vp, vp, i64, vp]
+        L.gevo_mx4_matmul.argtypes = [vp] * 10
         L.gevo_cnn_destroy.argtypes = [vp]
         L.gevo_cnn_destroy.restype = None
         L.gevo_pop_destroy.argtypes = [vp]
@@ -407,6 +422,23 @@ class Population:
         assert p.size == param_count(self.dims)
         _check(lib().gevo_pop_import(self._h, v, _fp(p)), "gevo_pop_import")
 
+    def layer_weights(self, layer: int, dtype=None):
+        """(w [P][d_l][d_{l-1}], b [P][d_l] float32) of layer 1 .. L of every
+        variant, as device tensors (gevo_pop_layer_weights); dtype torch.float32
+        or torch.bfloat16, by default the population's."""
+        torch = self.torch
+        if dtype is None:
+            dtype = torch.bfloat16 if self._cfg.dtype == BF16 else torch.float32
+        if not 1 <= layer < len(self.dims) or dtype not in (torch.float32, torch.bfloat16):
+            raise GevoError(f"layer_weights: layer {layer} of {len(self.dims) - 1}, {dtype}")
+        K, N = self.dims[layer - 1], self.dims[layer]
+        with torch.cuda.stream(self.stream):
+            w = torch.empty((self.P, N, K), dtype=dtype, device=self.workspace.device)
+            b = torch.empty((self.P, N), dtype=torch.float32, device=self.workspace.device)
+        _check(lib().gevo_pop_layer_weights(self._h, layer, BF16 if dtype == torch.bfloat16 else F32, w.data_ptr(),
+                                            b.data_ptr()), "gevo_pop_layer_weights")
+        return w, b
+
     def epoch_labels(self) -> np.ndarray:
         out = np.zeros(self.n_train, np.int32)
         _check(lib().gevo_pop_epoch_labels(self._h, out.ctypes.data_as(ctypes.POINTER(ctypes.c_int32)),
@@ -565,3 +597,20 @@ def _cnn_bias_count(cfg: dict) -> int:
         n += c + co
         c = co
     return n + cfg["classes"]
+
+
+_OPERATORS = ("Mx4", "RoutePlan", "expert_backward", "expert_combine", "expert_combine_backward", "expert_forward",
+              "mx4_matmul", "mx4_quantize", "route", "route_backward", "route_plan")
+
+
+def __getattr__(name):
+    """The operators of operators.py, which imports torch, at their first use."""
+    if name in _OPERATORS:
+        from . import operators
+        for n in _OPERATORS:
+            globals()[n] = getattr(operators, n)
+        return globals()[name]
+    raise AttributeError(f"module {__name__!r} has no attribute {name!r}")
+
+
+__all__ += _OPERATORS

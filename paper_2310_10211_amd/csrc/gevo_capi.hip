@@ -1541,6 +1541,21 @@ gevo_status gevo_pop_export(gevo_pop* p, uint32_t v, float* params_out, uint8_t*
   return GEVO_OK;
 }
 
+gevo_status gevo_pop_layer_weights(gevo_pop* p, uint32_t layer, gevo_dtype dtype, void* w, float* b) {
+  if (!p || layer < 1 || layer > (uint32_t)p->y.L || (dtype != GEVO_F32 && dtype != GEVO_BF16)) return GEVO_E_ARG;
+  if ((uintptr_t)w % (dtype == GEVO_BF16 ? 2 : 4) || (uintptr_t)b % 4) return GEVO_E_ARG;
+  const OnDevice on(p->device);
+  const gevo_status st = sync_masters(p);
+  if (st != GEVO_OK) return st;
+  const LayerLay& q = p->y.lay[layer - 1];
+  LayerWeightsArgs a{};
+  a.P = p->y.P; a.K = q.K; a.N = q.N; a.Kp = q.Kp; a.Np = q.Np; a.bf16 = dtype == GEVO_BF16;
+  a.Wm = at<float>(p, q.Wm); a.bias = at<float>(p, q.bias);
+  a.w = w; a.b = b;
+  if (w || b) HIP_TRY(launch_layer_weights(a, p->stream));
+  return GEVO_OK;
+}
+
 gevo_status gevo_pop_import(gevo_pop* p, uint32_t v, const float* params) {
   if (!p || !params) return GEVO_E_ARG;
   const Layout& y = p->y;

@@ -311,6 +311,13 @@ struct ExportArgs {
   float* params; uint8_t* mask_out;
 };
 hipError_t launch_export(const ExportArgs& a, hipStream_t s);
+// One layer of every variant: k-blocked masters -> [P][N][K] (float, or bf16 bits) and [P][N]
+struct LayerWeightsArgs {
+  int P, K, N, Kp, Np, bf16;
+  const float* Wm; const float* bias;
+  void* w; float* b;             // either nullable
+};
+hipError_t launch_layer_weights(const LayerWeightsArgs& a, hipStream_t s);
 hipError_t launch_zero_bytes(void* p, size_t bytes, hipStream_t s, const LaunchEv& ev);
 hipError_t launch_fused2(const Fused2Args& a, int P, hipStream_t s, const LaunchEv& ev);
 // W1 master of a two-layer net: k-blocked layout <-> the fused kernel's register image

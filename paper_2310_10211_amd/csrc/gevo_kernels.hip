@@ -1150,6 +1150,22 @@ __global__ __launch_bounds__(256) void k_export(ExportArgs a) {
   if (kb == 0 && y == 0) a.params[(size_t)a.K * a.N + n] = a.bias[n];
 }
 
+// A thread: one weight of one variant, consecutive ones a unit's inputs, which
+// are consecutive in the master 32 at a time.  Bound by the copy's bytes.
+__global__ __launch_bounds__(256) void k_layer_weights(LayerWeightsArgs a) {
+  const int k = blockIdx.x * 256 + threadIdx.x, n = blockIdx.y;
+  if (k >= a.K) return;
+  for (int v = blockIdx.z; v < a.P; v += gridDim.z) {
+    if (a.w) {
+      const float f = a.Wm[(((size_t)v * (a.Kp / 32) + k / 32) * a.Np + n) * 32 + k % 32];
+      const size_t at = ((size_t)v * a.N + n) * a.K + k;
+      if (a.bf16) ((uint16_t*)a.w)[at] = f32_to_bf16_bits(f);
+      else ((float*)a.w)[at] = f;
+    }
+    if (a.b && k == 0) a.b[(size_t)v * a.N + n] = a.bias[(size_t)v * a.Np + n];
+  }
+}
+
 __global__ __launch_bounds__(256) void k_reduce_partials(const double* part_ce, const unsigned int* part_corr,
                                                          int P, int nch, double* ce_out,
                                                          unsigned long long* corr_out) {
@@ -1299,6 +1315,12 @@ hipError_t launch_zero_bytes(void* p, size_t bytes, hipStream_t s, const LaunchE
 hipError_t launch_export(const ExportArgs& a, hipStream_t s) {
   if (a.Kp % 32 || a.Np % 32 || a.K > a.Kp || a.N > a.Np) return hipErrorInvalidValue;
   hipLaunchKernelGGL(k_export, dim3(a.Kp / 32, a.Np / 32), dim3(256), 0, s, a);
+  return hipGetLastError();
+}
+
+hipError_t launch_layer_weights(const LayerWeightsArgs& a, hipStream_t s) {
+  if (a.K > a.Kp || a.N > a.Np) return hipErrorInvalidValue;
+  hipLaunchKernelGGL(k_layer_weights, dim3((a.K + 255) / 256, a.N, a.P < 4096 ? a.P : 4096), dim3(256), 0, s, a);
   return hipGetLastError();
 }
 
