@@ -603,7 +603,7 @@ gevo_status gevo_route_backward(const gevo_route_config* cfg, const void* d_logi
  *   offsets[E + 1]  expert e's sorted rows are offsets[e] .. offsets[e + 1)
  *   order[slots]    slot of each sorted row; entries from offsets[E] on are left
  *   pos[slots]      sorted row of each slot, -1 where the id is outside [0, E)
- * d_ws: gevo_route_plan_bytes bytes, 4-byte aligned.
+ * d_ws: gevo_route_plan_bytes bytes, 4-byte aligned (for a few slots 0, and NULL).
  */
 gevo_status gevo_route_plan_bytes(int64_t slots, uint32_t E, size_t* bytes);
 gevo_status gevo_route_plan(int64_t slots, uint32_t E, const int32_t* d_ids, void* d_ws, size_t ws_bytes,

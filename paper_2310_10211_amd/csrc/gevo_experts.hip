@@ -2,24 +2,22 @@
 // (sorted by expert, gathered from x; or every row for every expert) times
 // W_e^T, with W_e [N][K], and the two products of its gradient.
 //
-// k_expert_tile computes a 128 x 256 tile of the output.  Operands of every
-// type pass through LDS alike, as rows of 64 bytes of contraction a step (16
-// fp32, 32 bf16, 128 4-bit values): 16-byte chunks, one a lane and matrix
-// instruction.  The order of the contraction inside a chunk is free as long as
-// both operands share it, so
+// k_expert_tile computes one tile of the output.  Operands of every type pass
+// through LDS alike, as rows of 64 bytes of contraction a step (16 fp32, 32
+// bf16, 128 4-bit values): 16-byte chunks, one a lane and matrix instruction.
+// The order of the contraction inside a chunk is free as long as both operands
+// share it, so
 //   bf16   a chunk is one operand of a 32x32x16 instruction,
 //   fp32   its four values feed four 32x32x2 instructions,
 //   4 bit  it is one block of 32 values, whose scale is one byte of the lane's
 //          scale operand in a 32x32x64 instruction.
-// Four waves of 64 x 128 read 24 KB of operands from LDS for 1,024 matrix
-// clocks of a step (96 of the 128 bytes a clock LDS gives; 64 x 64 a wave would
-// ask for all of them).  Three buffers of 24 KB hold a step in use and two
-// under way, and leave room for two workgroups on a CU.
+// Three buffers hold a step in use and two under way.
 #include "gevo_internal.h"
 #include "gevo_device.h"
 #include "gevo_ops.h"
 
 #include <type_traits>
+#include <stdlib.h>  //TUNE
 
 namespace gevo {
 
@@ -28,11 +26,31 @@ namespace {
 typedef int i32x8_t __attribute__((ext_vector_type(8)));
 typedef float f32x4_t __attribute__((ext_vector_type(4)));
 
-constexpr int kXR = 128, kWR = 256;              // rows of the two operand tiles
-constexpr int kStep = 64;                        // bytes of contraction a step
-constexpr int kBufs = 3;
-constexpr int kXBytes = kXR * kStep, kWBytes = kWR * kStep;
-constexpr int kScaleBytes = (kXR + kWR) * 4;
+// A workgroup's tile: RM x RN waves of (32 MI) x (32 NI), in steps of STEP
+// bytes of contraction, WGS workgroups on a CU.
+//   Wide   256 x 256, eight waves: per matrix clock of a step 32 bytes of
+//          operands from memory to LDS (a CU takes in about 47 of such loads)
+//          and 96 from LDS to the waves
+//   Mid    128 x 128
+//   Small  64 x 64: products of few tiles, spread over more of the chip
+// Two buffers hold a step in use and one under way.  Steps of 128 bytes read
+// whole cache lines; the squares of transposed fp32 operands allow 64.
+template <int RM_, int RN_, int MI_, int NI_, int WGS_, int STEP_>
+struct Shape {
+  static constexpr int RM = RM_, RN = RN_, MI = MI_, NI = NI_, WGS = WGS_;
+  static constexpr int kStep = STEP_;                // bytes of contraction a step
+  static constexpr int kThreads = 64 * RM * RN, kWaves = RM * RN;
+  static constexpr int kXR = RM * 32 * MI, kWR = RN * 32 * NI;
+  static constexpr int kXBytes = kXR * kStep, kWBytes = kWR * kStep;
+  static constexpr int kLoadRows = 1024 / kStep;     // of a wave's load
+  static constexpr int kXL = kXR / kLoadRows / kWaves, kWL = kWR / kLoadRows / kWaves;   // loads a wave and step
+  static constexpr int kScaleBytes = (kXR + kWR) * (kStep / 16);
+};
+template <ExpertType TY> struct Shapes {
+  typedef Shape<4, 2, 2, 4, 1, TY == kTypeF32 ? 64 : 128> Wide;
+  typedef Shape<2, 2, 2, 2, 3, 64> Mid;
+  typedef Shape<2, 2, 1, 1, 4, 128> Small;
+};
 
 __device__ uint4 g_zero_chunk;                   // what a chunk outside an operand reads
 
@@ -101,9 +119,21 @@ __device__ __forceinline__ void dma4_at(const void* p, uint32_t lds) {
       : "memory");
 }
 
+// A wave-uniform value in a scalar register, wherever the compiler holds it.
+// (The wait is for a vector write of v just before, which the compiler does not
+// know the lane read of.)
+__device__ __forceinline__ uint32_t scalar(uint32_t v) {
+  uint32_t s;
+  asm volatile("s_nop 1\n\tv_readfirstlane_b32 %0, %1" : "=s"(s) : "v"(v));
+  return s;
+}
+
 // Chunk c of row r of an operand tile lies at chunk c ^ turn(r) of the row: any
 // 8 or 16 consecutive rows then cover the banks once.
-__device__ __forceinline__ int turn(int r) { return (r & 4) >> 1 | (((r >> 1) ^ (r >> 3)) & 1); }
+template <int STEP>
+__device__ __forceinline__ int turn(int r) {
+  return STEP == 128 ? (r >> 1) & 7 : ((r & 4) >> 1 | (((r >> 1) ^ (r >> 3)) & 1));
+}
 
 // rows of segment e, kept inside [0, S]
 __device__ __forceinline__ void segment(const ExpertArgs& a, int e, int64_t& s0, int64_t& cnt) {
@@ -127,15 +157,16 @@ __device__ __forceinline__ int64_t source_row(const ExpertArgs& a, int64_t s0, i
   return a.offsets ? placed_row(a.order, a.k, a.xrows, s0 + i) : i;
 }
 
-// Workgroup -> tile of a list that runs expert by expert, each expert's tiles
-// column tile by column tile with the row tiles fastest.  XCD j (workgroups
-// with index j mod 8) gets the j-th eighth of the list, so the tiles that read
-// one weight tile run near each other under one L2.  Every wave sums the
+// Workgroup -> tile of a list, of which XCD j (workgroups with index j mod 8)
+// gets the j-th eighth, so that the tiles that read the same operands run near
+// each other under one L2.  Routed rows: expert by expert, each expert's tiles
+// column tile by column tile with the row tiles fastest.  Every wave sums the
 // experts' tile counts, 64 at a time.
 struct Tile {
   int e, nt;
   int64_t s0, cnt, m0;
 };
+template <int kXR>
 __device__ __forceinline__ bool find_tile(const ExpertArgs& a, int ntiles, Tile& o) {
   const int lane = threadIdx.x & 63;
   uint32_t total = 0;
@@ -151,7 +182,7 @@ __device__ __forceinline__ bool find_tile(const ExpertArgs& a, int ntiles, Tile&
       if (lane >= d) inc += v;
     }
     before = inc - mine;
-    return (uint32_t)__shfl((int)inc, 63, 64);
+    return (uint32_t)__builtin_amdgcn_readlane((int)inc, 63);
   };
   if (a.offsets) {
     for (int b = 0; b < a.E; b += 64) total += look(b);
@@ -162,20 +193,28 @@ __device__ __forceinline__ bool find_tile(const ExpertArgs& a, int ntiles, Tile&
   uint32_t idx = (blockIdx.x & 7) * each + at;
   if (at >= each || idx >= total) return false;
   if (!a.offsets) {
-    const uint32_t per = total / (uint32_t)a.E;
-    o.e = (int)(idx / per);
-    idx -= (uint32_t)o.e * per;
+    // Every matrix's rows are the same: an eighth of the row tiles goes to each
+    // XCD for all matrices, so that these rows stay in its L2 and the matrices
+    // pass by (64 variants of 784-512 over 10,000 rows in 4 bits 327 us;
+    // an eighth of the matrices to each XCD, as where rows differ, 343).
+    const uint32_t rts = (uint32_t)((a.M + kXR - 1) / kXR), all = (uint32_t)a.E * (uint32_t)ntiles;
+    const uint32_t group = a.x_e == 0 ? (rts + 7) / 8 : rts, g = idx / (group * all);
+    idx -= g * group * all;
+    const uint32_t here = min(group, rts - g * group), c = idx / here;
+    o.e = __builtin_amdgcn_readfirstlane((int)(c / (uint32_t)ntiles));
+    o.nt = __builtin_amdgcn_readfirstlane((int)(c % (uint32_t)ntiles));
+    o.m0 = (int64_t)(g * group + __builtin_amdgcn_readfirstlane((int)(idx % here))) * kXR;
+    segment(a, o.e, o.s0, o.cnt);
+    return true;
   } else {
     for (int b = 0;; b += 64) {
       if (b >= a.E) return false;
-      uint32_t sum;
-      if (a.E > 64 || b > 0) sum = look(b);
-      else sum = total;                              // still in the lanes
+      const uint32_t sum = a.E > 64 ? look(b) : total;   // (up to 64: still in the lanes)
       if (idx < sum) {
         const uint64_t in = __ballot(idx >= before && idx < before + mine);
         const int l = __ffsll((unsigned long long)in) - 1;
         o.e = b + l;
-        idx -= (uint32_t)__shfl((int)before, l, 64);
+        idx -= (uint32_t)__builtin_amdgcn_readlane((int)before, __builtin_amdgcn_readfirstlane(l));
         break;
       }
       idx -= sum;
@@ -190,16 +229,20 @@ __device__ __forceinline__ bool find_tile(const ExpertArgs& a, int ntiles, Tile&
   return true;
 }
 
-// 16 bytes at p of which the first `valid` elements exist; whole: one load
+// 16 bytes at p, which has its element's alignment, of which the first `valid`
+// elements exist
 template <typename S>
-__device__ __forceinline__ uint4 load_chunk(const char* p, int valid, bool whole) {
+__device__ __forceinline__ uint4 load_chunk(const char* p, int valid) {
   constexpr int V = 16 / sizeof(S);
   if (valid <= 0) return make_uint4(0, 0, 0, 0);
-  if (whole && valid >= V) return *reinterpret_cast<const uint4*>(p);
+  uint4 u;
+  if (valid >= V) {
+    __builtin_memcpy(&u, p, 16);                     // one load, at any address
+    return u;
+  }
   S e[V];
 #pragma unroll
   for (int i = 0; i < V; ++i) e[i] = i < valid ? reinterpret_cast<const S*>(p)[i] : (S)0;
-  uint4 u;
   __builtin_memcpy(&u, e, 16);
   return u;
 }
@@ -209,34 +252,43 @@ enum Pass { kForward, kDx, kDw };
 
 }  // namespace
 
-// A tile of a product.  XL, WL: how the operand tiles reach LDS.
-//   kDma         16-byte chunks straight to LDS, two steps ahead
-//   kGuarded     through registers, element by element where rows are not
-//                aligned or the contraction ends inside a chunk
+// Tiles of a product.  XL, WL: how the operand tiles reach LDS.
+//   kDma         16-byte chunks straight to LDS, a step ahead
+//   kGuarded     through registers, at any address, where rows are not aligned
+//                or the contraction ends inside a chunk
 //   kTransposed  the contraction is the operand's outer index: a lane loads a
 //                square of 8 x 8 (fp32: 4 x 4) values and turns it in registers
-template <ExpertType TY, Pass PASS, Load XL, Load WL, bool OUT16>
-__global__ __launch_bounds__(256, 2) void k_expert_tile(ExpertArgs a) {
+template <typename SH, ExpertType TY, Pass PASS, Load XL, Load WL, bool OUT16>
+__global__ __launch_bounds__(SH::kThreads, SH::WGS* SH::kThreads / 256) void k_expert_tile(ExpertArgs a) {
   typedef Mm<TY> M;
   typedef typename M::S S;
+  typedef typename std::conditional<OUT16, uint16_t, float>::type O;
+  constexpr int kXR = SH::kXR, kWR = SH::kWR, kXBytes = SH::kXBytes, kWBytes = SH::kWBytes;
+  constexpr int MI = SH::MI, NI = SH::NI, NXL = SH::kXL, NWL = SH::kWL, kLR = SH::kLoadRows;
   constexpr int V = 16 / sizeof(S);                  // elements a chunk (not of 4-bit operands)
+  constexpr int kStep = SH::kStep, kC = kStep / 16, kQ = kStep / 32;   // chunks, parts of a step
   constexpr bool mx = TY == kTypeMx4;
-  constexpr int kBuf = kXBytes + kWBytes + (mx ? kScaleBytes : 0);
+  constexpr int kBuf = kXBytes + kWBytes + (mx ? SH::kScaleBytes : 0);
   constexpr bool kAllDma = XL == kDma && WL == kDma;
-  constexpr int kIssued = (XL == kDma ? 2 : 0) + (WL == kDma ? 4 : 0) + (mx ? 2 : 0);   // loads to LDS a step and wave
+  constexpr int kIssued = (XL == kDma ? NXL : 0) + (WL == kDma ? NWL : 0) + (mx ? kC / 4 : 0);   // a step and wave
   extern __shared__ __align__(16) char smem[];
 
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l32 = lane & 31, lh = lane >> 5;
   const int wu = __builtin_amdgcn_readfirstlane(wave);
-  const int wm = wave & 1, wn = wave >> 1;           // 64-row, 128-column band of the wave
+  // the wave's band of rows and of columns; the waves of a band sit on
+  // different SIMDs, so bands without rows leave their share to the others
+  const int wm = wu / SH::RN, wn = wu % SH::RN;
   const uint32_t lds0 = lds_addr(smem);
+  const int cols = PASS == kDw ? a.K : a.N;          // of the output
+  const int bytes = mx ? (a.K + 127) / 128 * 64 : a.K * (int)sizeof(S);   // of a contraction row (not kDw)
+  constexpr int kPer = mx ? 2 * kStep : kStep / (int)sizeof(S);           // elements a step
 
   Tile tl;
   if constexpr (PASS == kDw) {
     // tiles of every expert's [N][K] gradient; x operand: columns of dy, w operand: columns of x
     const int nr = (a.N + kXR - 1) / kXR, nc = (a.K + kWR - 1) / kWR;
-    const uint32_t total = (uint32_t)a.E * (uint32_t)(nr * nc), each = (total + 7) / 8, at = blockIdx.x >> 3;
-    const uint32_t idx = (blockIdx.x & 7) * each + at;
+    const uint32_t total = (uint32_t)a.E * (uint32_t)(nr * nc), each = (total + 7) / 8;
+    const uint32_t at = blockIdx.x >> 3, idx = (blockIdx.x & 7) * each + at;
     if (at >= each || idx >= total) return;
     tl.e = (int)(idx / (uint32_t)(nr * nc));
     const int in = (int)(idx % (uint32_t)(nr * nc));
@@ -244,284 +296,346 @@ __global__ __launch_bounds__(256, 2) void k_expert_tile(ExpertArgs a) {
     tl.m0 = (int64_t)(in % nr) * kXR;
     segment(a, tl.e, tl.s0, tl.cnt);
   } else {
-    if (!find_tile(a, (a.N + kWR - 1) / kWR, tl)) return;
+    if (!find_tile<kXR>(a, (a.N + kWR - 1) / kWR, tl)) return;
   }
   const int n0 = tl.nt * kWR;
-  const int cols = PASS == kDw ? a.K : a.N;          // of the output
+  const int64_t rows = PASS == kDw ? a.N : tl.cnt;
+  const bool has_rows = tl.m0 + wm * 32 * MI < rows && n0 + wn * 32 * NI < cols;   // the wave's part of the output
+  const int64_t clen = PASS == kDw ? tl.cnt : a.K;   // contraction, elements
+  const int nst = (int)((clen + kPer - 1) / kPer);   // steps
 
-  // contraction: elements (steps of kStep bytes), chunks past `bytes` read zeros
-  const int64_t clen = PASS == kDw ? tl.cnt : a.K;
-  constexpr int kPer = mx ? 2 * kStep : kStep / (int)sizeof(S);   // elements a step
-  const int nst = (int)((clen + kPer - 1) / kPer);
-  const int bytes = mx ? (int)((a.K + 127) / 128 * 64) : (int)(a.K * (int64_t)sizeof(S));   // (not kDw)
-
-  // ---- chunks in row order: rows 16 j + lane / 4, chunk lane % 4 of LDS
-  const int crow16 = lane >> 2, cbyte = 16 * ((lane & 3) ^ turn(crow16));
-  const char* xp[2];
-  int xlim[2];
-  const char* wp[4];
-  int wlim[4];
-  if constexpr (XL != kTransposed) {
-#pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      const int64_t i = tl.m0 + 16 * (2 * wave + j) + crow16;
-      int64_t r = i < tl.cnt ? source_row(a, tl.s0, i) : -1;
-      xlim[j] = r >= 0 ? bytes : 0;
-      if (r < 0) r = 0;
-      xp[j] = (const char*)a.x + (a.offsets ? 0 : tl.e * a.x_e) + r * a.x_stride + cbyte;
-    }
-  }
-  if constexpr (WL != kTransposed) {
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int n = n0 + 16 * (4 * wave + j) + crow16;
-      wlim[j] = n < a.N ? bytes : 0;
-      wp[j] = (const char*)a.w + tl.e * a.w_e + (n < a.N ? n : 0) * a.w_n + cbyte;
-    }
-  }
-  const char* xsp = nullptr;
-  const char* wsp = nullptr;
-  if constexpr (mx) {                                // a wave loads 64 rows' scales of each operand, 4 bytes a step
-    const int64_t i = tl.m0 + 64 * (wave & 1) + lane;
-    const int64_t r = i < tl.cnt ? source_row(a, tl.s0, i) : -1;
-    if (r >= 0) xsp = (const char*)a.xs + (a.offsets ? 0 : tl.e * a.xs_e) + r * a.xs_stride;
-    const int n = n0 + 64 * wave + lane;
-    if (n < a.N) wsp = (const char*)a.ws + tl.e * a.ws_e + n * a.ws_n;
-  }
+  // ---- chunks in row order: a load's rows follow each other, kC lanes a row.
+  // A row's turn is the same in every second load.
+  const int crow = lane / kC;
+  const int cb[2] = {16 * ((lane % kC) ^ turn<kStep>(crow)), 16 * ((lane % kC) ^ turn<kStep>(kLR + crow))};
+  const char* xp[NXL];
+  const char* wp[NWL];
+  uint32_t have = 0;                                 // bit j: load j of x has a row, bit 16 + j: of w
   const char* zero = (const char*)&g_zero_chunk;
-  auto issue = [&](int st) {
-    const uint32_t buf = lds0 + (uint32_t)(st % kBufs) * kBuf;
-    const int at = st * kStep;
-    if constexpr (XL == kDma) {
+  const char* sp = nullptr;                          // 4-bit operands: a wave loads 64 rows' scales
+  constexpr int kSx = kXR / 64, kSn = (kXR + kWR) / 64;
+  const int sj = wu % kSn;
+  static_assert(!mx || SH::kWaves >= kSn, "every row's scales have a wave");
+
+  // ---- transposed: squares of V contraction rows x V columns, one a thread,
+  // the w tile's first.  A square's V chunks are one chunk column of V rows of
+  // the tile.
+  constexpr bool kTr = XL == kTransposed || WL == kTransposed;
+  constexpr int kWsq = WL == kTransposed ? kWR / V * kC : 0, kXsq = XL == kTransposed ? kXR / V * kC : 0;
+  static_assert(kWsq + kXsq <= SH::kThreads, "one square a thread");
+  uint4 sq[kTr ? V : 1];
+  const bool sq_x = tid >= kWsq, sq_live = tid < kWsq + kXsq;
+  const int sq_id = sq_x ? tid - kWsq : tid, sq_kc = sq_id % kC, sq_r0 = sq_id / kC * V;
+  const char* sq_p = nullptr;                        // contraction row 0, the square's first column
+  int64_t sq_stride = 0;
+  int sq_valid = 0;                                  // columns that exist
+  int32_t sq_row[kTr ? V : 1];                       // rows of the step to fetch next
+  float dbs[V];
+
+  {
+    if constexpr (XL != kTransposed) {
 #pragma unroll
-      for (int j = 0; j < 2; ++j)
-        dma16_at(at + cbyte < xlim[j] ? xp[j] + at : zero, buf + (uint32_t)(2 * wu + j) * 1024u);
+      for (int j = 0; j < NXL; ++j) {
+        const int64_t i = tl.m0 + kLR * (NXL * wave + j) + crow;
+        int64_t r = i < tl.cnt ? source_row(a, tl.s0, i) : -1;
+        if (r >= 0) have |= 1u << j;
+        else r = 0;
+        xp[j] = (const char*)a.x + (a.offsets ? 0 : tl.e * a.x_e) + r * a.x_stride + cb[j & 1];
+      }
     }
-    if constexpr (WL == kDma) {
+    if constexpr (WL != kTransposed) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
-        dma16_at(at + cbyte < wlim[j] ? wp[j] + at : zero, buf + kXBytes + (uint32_t)(4 * wu + j) * 1024u);
+      for (int j = 0; j < NWL; ++j) {
+        const int n = n0 + kLR * (NWL * wave + j) + crow;
+        if (n < a.N) have |= 0x10000u << j;
+        wp[j] = (const char*)a.w + tl.e * a.w_e + (n < a.N ? n : 0) * a.w_n + cb[j & 1];
+      }
     }
     if constexpr (mx) {
-      dma4_at(xsp ? xsp + st * 4 : zero, buf + kXBytes + kWBytes + (uint32_t)(wu & 1) * 256u);
-      dma4_at(wsp ? wsp + st * 4 : zero, buf + kXBytes + kWBytes + kXR * 4 + (uint32_t)wu * 256u);
+      sp = nullptr;
+      if (sj < kSx) {
+        const int64_t i = tl.m0 + 64 * sj + lane;
+        const int64_t r = i < tl.cnt ? source_row(a, tl.s0, i) : -1;
+        if (r >= 0) sp = (const char*)a.xs + (a.offsets ? 0 : tl.e * a.xs_e) + r * a.xs_stride;
+      } else {
+        const int n = n0 + 64 * (sj - kSx) + lane;
+        if (n < a.N) sp = (const char*)a.ws + tl.e * a.ws_e + n * a.ws_n;
+      }
     }
+    if constexpr (kTr) {
+      const int c = (PASS == kDw && sq_x ? (int)tl.m0 : n0) + sq_r0;
+      if (PASS == kDx) {                             // columns of W_e, contraction over its rows
+        sq_p = (const char*)a.w + tl.e * a.w_e;
+        sq_stride = a.w_n;
+        sq_valid = a.N - c;
+      } else if (sq_x) {                             // dw: columns of dy
+        sq_p = (const char*)a.w + tl.s0 * a.w_n;
+        sq_stride = a.w_n;
+        sq_valid = a.N - c;
+      } else {                                       // dw: columns of x, gathered rows
+        sq_p = (const char*)a.x;
+        sq_stride = a.x_stride;
+        sq_valid = a.K - c;
+      }
+      if (!sq_live || sq_valid < 0) sq_valid = 0;
+      sq_p += (size_t)c * sizeof(S);
+    }
+  }
+
+  // load n of the wave's kIssued loads of step st, to buffer b
+  auto issue_one = [&](int st, int b, int n) {
+    const uint32_t buf = scalar(lds0 + (uint32_t)b * kBuf);
+    const int at = st * kStep;
+    if (XL == kDma && n < NXL) {
+      const bool in = (have >> n & 1) && at + cb[n & 1] < bytes;
+      dma16_at(in ? xp[n] + at : zero, buf + (uint32_t)(NXL * wu + n) * 1024u);
+      return;
+    }
+    if (XL == kDma) n -= NXL;
+    if (WL == kDma && n < NWL) {
+      const bool in = (have >> (16 + n) & 1) && at + cb[n & 1] < bytes;
+      dma16_at(in ? wp[n] + at : zero, buf + kXBytes + (uint32_t)(NWL * wu + n) * 1024u);
+      return;
+    }
+    if (WL == kDma) n -= NWL;
+    if constexpr (mx)
+      dma4_at(sp && st * kC + n * 4 < bytes / 16 ? sp + st * kC + n * 4 : zero,
+              buf + kXBytes + kWBytes + (uint32_t)n * (kXR + kWR) * 4u + (uint32_t)sj * 256u);
+  };
+  auto issue = [&](int st, int b) {
+#pragma unroll
+    for (int n = 0; n < kIssued; ++n) issue_one(st, b, n);
   };
 
-  // ---- chunks through registers
-  uint4 xg[XL == kGuarded ? 2 : 1], wg[WL == kGuarded ? 4 : 1];
-  const bool xwhole = ((uintptr_t)a.x | (uintptr_t)a.x_stride) % 16 == 0;
-  const bool wwhole = ((uintptr_t)a.w | (uintptr_t)a.w_e | (uintptr_t)a.w_n) % 16 == 0;
+  // ---- through registers: step st from memory, and to buffer b
+  uint4 xg[XL == kGuarded ? NXL : 1], wg[WL == kGuarded ? NWL : 1];
+  auto place = [&](int st) {                         // rows of a step's squares
+    if constexpr (kTr) {
+#pragma unroll
+      for (int i = 0; i < V; ++i) {
+        const int k = st * kPer + sq_kc * V + i;
+        sq_row[i] = k < clen && sq_valid > 0 ? k : -1;
+        if (PASS == kDw && !sq_x && sq_row[i] >= 0) sq_row[i] = (int)source_row(a, tl.s0, k);
+      }
+    }
+  };
   auto fetch = [&](int st) {
     const int at = st * kStep;
     if constexpr (XL == kGuarded) {
 #pragma unroll
-      for (int j = 0; j < 2; ++j)
-        xg[j] = load_chunk<S>(xp[j] + at, (xlim[j] - at - cbyte) / (int)sizeof(S), xwhole);
+      for (int j = 0; j < NXL; ++j)
+        xg[j] = load_chunk<S>(xp[j] + at, have >> j & 1 ? (bytes - at - cb[j & 1]) / (int)sizeof(S) : 0);
     }
     if constexpr (WL == kGuarded) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j)
-        wg[j] = load_chunk<S>(wp[j] + at, (wlim[j] - at - cbyte) / (int)sizeof(S), wwhole);
+      for (int j = 0; j < NWL; ++j)
+        wg[j] = load_chunk<S>(wp[j] + at, have >> (16 + j) & 1 ? (bytes - at - cb[j & 1]) / (int)sizeof(S) : 0);
+    }
+    if constexpr (kTr) {
+#pragma unroll
+      for (int i = 0; i < V; ++i)
+        sq[i] = load_chunk<S>(sq_p + (sq_row[i] < 0 ? 0 : sq_row[i]) * sq_stride, sq_row[i] < 0 ? 0 : sq_valid);
     }
   };
-  auto put = [&](int st) {
-    char* buf = smem + (size_t)(st % kBufs) * kBuf;
+  auto put = [&](int b, bool sums) {
+    char* buf = smem + b * kBuf;
     if constexpr (XL == kGuarded) {
 #pragma unroll
-      for (int j = 0; j < 2; ++j) *reinterpret_cast<uint4*>(buf + (2 * wave + j) * 1024 + lane * 16) = xg[j];
+      for (int j = 0; j < NXL; ++j) *reinterpret_cast<uint4*>(buf + (NXL * wave + j) * 1024 + lane * 16) = xg[j];
     }
     if constexpr (WL == kGuarded) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) *reinterpret_cast<uint4*>(buf + kXBytes + (4 * wave + j) * 1024 + lane * 16) = wg[j];
+      for (int j = 0; j < NWL; ++j)
+        *reinterpret_cast<uint4*>(buf + kXBytes + (NWL * wave + j) * 1024 + lane * 16) = wg[j];
     }
-  };
-
-  // ---- transposed: squares of V contraction rows x V columns.  A square's V
-  // chunks are one chunk column of V rows of the tile.  bf16: the w tile's 128
-  // squares go to threads 0-127, the x tile's 64 to 128-191; fp32: 256 and 128,
-  // two to a thread.
-  constexpr bool kTr = XL == kTransposed || WL == kTransposed;
-  constexpr int kSq = !kTr ? 0 : (V == 8 ? 1 : (XL == kTransposed ? 2 : 1));
-  uint4 sq[kSq ? kSq : 1][V];
-  struct Square {
-    const char* p;           // contraction row 0, first column
-    int64_t stride;          // bytes between contraction rows
-    int valid, row, lds;     // columns that exist; first contraction row in a step; place in the buffer
-    bool whole, gather, isx;
-  } sd[kSq ? kSq : 1];
-  float dbs[V];
-#pragma unroll
-  for (int v = 0; v < V; ++v) dbs[v] = 0.0f;
-  if constexpr (kTr) {
-#pragma unroll
-    for (int q = 0; q < kSq; ++q) {
-      Square& d = sd[q];
-      constexpr int wsq = kWR / V * 4, xsq = kXR / V * 4;
-      const int b = V == 8 ? tid : tid;
-      bool isx = V == 8 ? (XL == kTransposed && b >= wsq) : q == 1;
-      const int id = V == 8 && isx ? b - wsq : b;
-      const bool live = id < (isx ? xsq : wsq) && (isx ? XL == kTransposed : WL == kTransposed);
-      const int kc = id & 3, r0 = (id >> 2) * V;     // chunk, first tile row
-      d.isx = isx;
-      d.row = kc * V;
-      d.lds = (isx ? 0 : kXBytes) + r0 * kStep;
-      d.gather = false;
-      if (PASS == kDx) {                             // w tile: columns n0 + r0 of W_e, contraction over its rows
-        const int c = n0 + r0;
-        d.valid = a.N - c;
-        d.p = (const char*)a.w + tl.e * a.w_e + (size_t)c * sizeof(S);
-        d.stride = a.w_n;
-        d.whole = wwhole;
-      } else if (isx) {                              // dw: columns of dy
-        const int c = (int)tl.m0 + r0;
-        d.valid = a.N - c;
-        d.p = (const char*)a.w + tl.s0 * a.w_n + (size_t)c * sizeof(S);
-        d.stride = a.w_n;
-        d.whole = ((uintptr_t)a.w | (uintptr_t)a.w_n) % 16 == 0;
-      } else {                                       // dw: columns of x, gathered rows
-        const int c = n0 + r0;
-        d.valid = a.K - c;
-        d.p = (const char*)a.x + (size_t)c * sizeof(S);
-        d.stride = a.x_stride;
-        d.whole = xwhole;
-        d.gather = true;
-      }
-      if (!live) d.valid = 0;
-    }
-  }
-  auto fetch_t = [&](int st) {
     if constexpr (kTr) {
+      if (!sq_live) return;
+      if (!sq_x) buf += kXBytes;
 #pragma unroll
-      for (int q = 0; q < kSq; ++q) {
-        const Square& d = sd[q];
-        int64_t row[V];
+      for (int c = 0; c < V; ++c) {
+        uint4 o;
+        if constexpr (V == 8) {
+          uint32_t w[4];
 #pragma unroll
-        for (int i = 0; i < V; ++i) {
-          const int64_t k = (int64_t)st * kPer + d.row + i;
-          row[i] = k < clen && d.valid > 0 ? k : -1;
-          if (PASS == kDw && d.gather && row[i] >= 0) row[i] = source_row(a, tl.s0, row[i]);
+          for (int p = 0; p < 4; ++p) {              // values c of contraction rows 2p, 2p + 1
+            const uint32_t lo = (&sq[2 * p].x)[c >> 1], hi = (&sq[2 * p + 1].x)[c >> 1];
+            w[p] = __builtin_amdgcn_perm(hi, lo, c & 1 ? 0x07060302u : 0x05040100u);
+          }
+          o = make_uint4(w[0], w[1], w[2], w[3]);
+        } else {
+          o = make_uint4((&sq[0].x)[c], (&sq[1].x)[c], (&sq[2].x)[c], (&sq[3].x)[c]);
         }
+        *reinterpret_cast<uint4*>(buf + (sq_r0 + c) * kStep + 16 * (sq_kc ^ turn<kStep>(sq_r0 + c))) = o;
+        if (PASS == kDw && sq_x && sums) {
+          S e[V];
+          __builtin_memcpy(e, &o, 16);
 #pragma unroll
-        for (int i = 0; i < V; ++i)
-          sq[q][i] = load_chunk<S>(d.p + (row[i] < 0 ? 0 : row[i]) * d.stride, row[i] < 0 ? 0 : d.valid, d.whole);
-      }
-    }
-  };
-  auto put_t = [&](int st) {
-    if constexpr (kTr) {
-      char* buf = smem + (size_t)(st % kBufs) * kBuf;
-#pragma unroll
-      for (int q = 0; q < kSq; ++q) {
-        const Square& d = sd[q];
-        const bool live = V == 8 ? tid < (XL == kTransposed ? 192 : 128) : (!d.isx || tid < 128);
-        if (!live) continue;
-        const int kc = d.row / V, r0 = (d.lds - (d.isx ? 0 : kXBytes)) / kStep;
-#pragma unroll
-        for (int c = 0; c < V; ++c) {
-          uint4 o;
-          if constexpr (V == 8) {
-            uint32_t w[4];
-#pragma unroll
-            for (int p = 0; p < 4; ++p) {            // values c of contraction rows 2p, 2p + 1
-              const uint32_t lo = (&sq[q][2 * p].x)[c >> 1], hi = (&sq[q][2 * p + 1].x)[c >> 1];
-              w[p] = __builtin_amdgcn_perm(hi, lo, c & 1 ? 0x07060302u : 0x05040100u);
-            }
-            o = make_uint4(w[0], w[1], w[2], w[3]);
-          } else {
-            o = make_uint4((&sq[q][0].x)[c], (&sq[q][1].x)[c], (&sq[q][2].x)[c], (&sq[q][3].x)[c]);
-          }
-          *reinterpret_cast<uint4*>(buf + d.lds + c * kStep + 16 * (kc ^ turn(r0 + c))) = o;
-          if (PASS == kDw && d.isx && a.db && tl.nt == 0) {
-            S e[V];
-            __builtin_memcpy(e, &o, 16);
-#pragma unroll
-            for (int i = 0; i < V; ++i) dbs[c] += Op<S>::to_f32(e[i]);
-          }
+          for (int i = 0; i < V; ++i) dbs[c] += Op<S>::to_f32(e[i]);
         }
       }
     }
   };
-
-  f32x16_t acc[2][4];
-#pragma unroll
-  for (int i = 0; i < 2; ++i)
-#pragma unroll
-    for (int t = 0; t < 4; ++t) acc[i][t] = zero16();
 
   // The tile is accumulated transposed (w operand's rows down): lane l holds
   // row 32 i + l % 32 of the wave's band and, in registers 4 q + r, columns
   // 32 t + 8 q + 4 (l / 32) + r.
-  auto compute = [&](int st) {
-    const char* buf = smem + (size_t)(st % kBufs) * kBuf;
-    const char* xb = buf + (wm * 64 + l32) * kStep;
-    const char* wb = buf + kXBytes + (wn * 128 + l32) * kStep;
-    const int tr = turn(l32);
-    uint32_t sx[2] = {0, 0}, sw[4] = {0, 0, 0, 0};
+  //
+  // A step has kQ parts of one chunk a lane and operand.  Each part's operands
+  // are read while the part before is multiplied, so the step's barrier sits
+  // before its last part: by then every wave has read the whole step, whose
+  // buffer takes a later step's load, and the next step has landed.
+  f32x16_t acc[MI][NI];
+  struct Frag {
+    uint4 x[MI], w[NI];
+  } fr[2];
+  uint32_t sx[2][MI], sw[2][NI];                     // scales: of two parts, and the next two's
+#pragma unroll
+  for (int b = 0; b < 2; ++b) {
+#pragma unroll
+    for (int i = 0; i < MI; ++i) sx[b][i] = 0;
+#pragma unroll
+    for (int t = 0; t < NI; ++t) sw[b][t] = 0;
+  }
+  const int tr = turn<kStep>(l32);
+  const char* xb = smem + (wm * 32 * MI + l32) * kStep;
+  const char* wb = smem + kXBytes + (wn * 32 * NI + l32) * kStep;
+  auto read_x = [&](int b, int h) {
+    const int at = b * kBuf + 16 * ((2 * h + lh) ^ tr);
+#pragma unroll
+    for (int i = 0; i < MI; ++i) fr[h & 1].x[i] = *reinterpret_cast<const uint4*>(xb + at + 32 * i * kStep);
     if constexpr (mx) {
-      const uint32_t* sp = reinterpret_cast<const uint32_t*>(buf + kXBytes + kWBytes);
+      if ((h & 1) == 0) {
+        const uint32_t* sc =
+            reinterpret_cast<const uint32_t*>(smem + b * kBuf + kXBytes + kWBytes) + (h >> 1) * (kXR + kWR);
 #pragma unroll
-      for (int i = 0; i < 2; ++i) sx[i] = sp[wm * 64 + 32 * i + l32] >> (8 * lh);
+        for (int i = 0; i < MI; ++i) sx[1][i] = sc[wm * 32 * MI + 32 * i + l32] >> (8 * lh);
 #pragma unroll
-      for (int t = 0; t < 4; ++t) sw[t] = sp[kXR + wn * 128 + 32 * t + l32] >> (8 * lh);
+        for (int t = 0; t < NI; ++t) sw[1][t] = sc[kXR + wn * 32 * NI + 32 * t + l32] >> (8 * lh);
+      }
     }
-    auto step = [&](auto sc) {
-      constexpr int s = decltype(sc)::value;
-      const int co = 16 * ((2 * s + lh) ^ tr);
-      uint4 fx[2], fw[4];
+  };
+  auto read_w = [&](int b, int h, int t) {
+    const int at = b * kBuf + 16 * ((2 * h + lh) ^ tr);
+    fr[h & 1].w[t] = *reinterpret_cast<const uint4*>(wb + at + 32 * t * kStep);
+  };
+  auto mul = [&](auto hc, int t) {
+    constexpr int h = decltype(hc)::value;
 #pragma unroll
-      for (int i = 0; i < 2; ++i) fx[i] = *reinterpret_cast<const uint4*>(xb + 32 * i * kStep + co);
+    for (int i = 0; i < MI; ++i)
+      acc[i][t] = M::template mma<2 * h>(fr[h].w[t], fr[h].x[i], acc[i][t], sw[0][t], sx[0][i]);
+  };
+  auto next_scales = [&]() {
+    if constexpr (mx) {
 #pragma unroll
-      for (int t = 0; t < 4; ++t) fw[t] = *reinterpret_cast<const uint4*>(wb + 32 * t * kStep + co);
+      for (int i = 0; i < MI; ++i) sx[0][i] = sx[1][i];
 #pragma unroll
-      for (int t = 0; t < 4; ++t)
-#pragma unroll
-        for (int i = 0; i < 2; ++i) acc[i][t] = M::template mma<2 * s>(fw[t], fx[i], acc[i][t], sw[t], sx[i]);
-    };
-    step(std::integral_constant<int, 0>{});
-    step(std::integral_constant<int, 1>{});
+      for (int t = 0; t < NI; ++t) sw[0][t] = sw[1][t];
+    }
   };
 
+  // output: rows of the wave's band pass through the wave's own part of LDS 32
+  // at a time, so that they leave in segments of up to 256 bytes
+  constexpr int kFit = kXBytes + kWBytes >= SH::kWaves * 32 * 256 ? 256 : 128;
+  constexpr int kRowB = NI * 32 * (int)sizeof(O) < kFit ? NI * 32 * (int)sizeof(O) : kFit;   // bytes of a row a round
+  constexpr int kTs = kRowB / (32 * (int)sizeof(O));                                         // column tiles a round
+  constexpr int kCh = kRowB / 16, kEl = 16 / (int)sizeof(O);
+  static_assert(SH::kWaves * 32 * kRowB <= kXBytes + kWBytes, "the output's staging fits a buffer");
+  float* bs = reinterpret_cast<float*>(smem + 2 * kBuf);       // the tile's biases
+  const bool biased = PASS == kForward && a.bias;
+  const bool whole = ((cols | (int)(a.out_stride % kEl)) & (kEl - 1)) == 0 && (uintptr_t)a.out % 16 == 0;
+
+  const bool sums = PASS == kDw && a.db && tl.nt == 0;
+  float bias = 0.0f;
+  if (biased && tid < kWR && n0 + tid < a.N) bias = a.bias[(int64_t)tl.e * a.N + n0 + tid];
+#pragma unroll
+  for (int v = 0; v < V; ++v) dbs[v] = 0.0f;
+#pragma unroll
+  for (int i = 0; i < MI; ++i)
+#pragma unroll
+    for (int t = 0; t < NI; ++t) acc[i][t] = zero16();
+
   if (nst > 0) {
-    issue(0);
-    if (nst > 1) issue(1);
+    issue(0, 0);
     if constexpr (!kAllDma) {
+      place(0);
       fetch(0);
-      fetch_t(0);
-      put(0);
-      put_t(0);
+      place(1);
+      put(0, sums);
+      if (nst > 1) {
+        fetch(1);
+        place(2);
+      }
+    }
+    if (nst > 1) issue(1, 1);
+    if (nst > 1) wait_vm<kIssued>();
+    else wait_vm<0>();
+    __syncthreads();
+    if (has_rows) {
+      read_x(0, 0);
+#pragma unroll
+      for (int t = 0; t < NI; ++t) read_w(0, 0, t);
     }
     for (int st = 0; st < nst; ++st) {
-      if (st + 1 < nst) wait_vm<kIssued>();
-      else wait_vm<0>();
-      __syncthreads();                               // step st is in LDS; step st - 1's buffer is free
-      if (st + 2 < nst) issue(st + 2);
-      if constexpr (!kAllDma) {
-        if (st + 1 < nst) {
-          fetch(st + 1);
-          fetch_t(st + 1);
+      const int b = st & 1;
+      const bool more = st + 1 < nst, ahead = st + 2 < nst;
+      // parts that hold a value (of 4-bit rows, whose last step is often half empty)
+      const int filled = mx && !more ? (bytes - st * kStep + 31) / 32 : kQ;
+      auto part = [&](auto hc) {                     // part h, reading part h + 1 of the step
+        constexpr int h = decltype(hc)::value;
+        if (mx && h >= filled) return;
+        if ((h & 1) == 0) next_scales();
+        read_x(b, h + 1);
+#pragma unroll
+        for (int t = 0; t < NI; ++t) {
+          read_w(b, h + 1, t);
+          mul(std::integral_constant<int, h & 1>{}, t);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      };
+      if (has_rows) {
+        part(std::integral_constant<int, 0>{});
+        if constexpr (kQ == 4) {
+          part(std::integral_constant<int, 1>{});
+          part(std::integral_constant<int, 2>{});
         }
       }
-      compute(st);
       if constexpr (!kAllDma) {
-        if (st + 1 < nst) {
-          put(st + 1);
-          put_t(st + 1);
+        if (more) put(b ^ 1, sums);
+      }
+      wait_vm<0>();
+      __syncthreads();
+      if constexpr (!kAllDma) {
+        if (ahead) {
+          fetch(st + 2);
+          place(st + 3);
         }
+      }
+      if (has_rows && (!mx || filled == kQ)) {
+        if (more) read_x(b ^ 1, 0);
+#pragma unroll
+        for (int t = 0; t < NI; ++t) {
+          if (more) read_w(b ^ 1, 0, t);
+          mul(std::integral_constant<int, 1>{}, t);
+          if (ahead) {
+#pragma unroll
+            for (int n = t * kIssued / NI; n < (t + 1) * kIssued / NI; ++n) issue_one(st + 2, b, n);
+          }
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      } else if (ahead) {
+        issue(st + 2, b);
       }
     }
   }
 
   if constexpr (PASS == kDw) {
-    if (a.db && tl.nt == 0) {                        // column sums of dy: the four chunk lanes of a square's rows
+    if (sums) {                                    // column sums of dy: the chunk lanes of a square's rows
 #pragma unroll
-      for (int v = 0; v < V; ++v) {
-        dbs[v] += __shfl_xor(dbs[v], 1, 64);
-        dbs[v] += __shfl_xor(dbs[v], 2, 64);
-      }
-      const int b = V == 8 ? tid - 128 : tid;
-      if (b >= 0 && b < kXR / V * 4 && (b & 3) == 0) {
-        const int c = (int)tl.m0 + (b >> 2) * V;
+      for (int v = 0; v < V; ++v)
+#pragma unroll
+        for (int m = 1; m < kC; m <<= 1) dbs[v] += __shfl_xor(dbs[v], m, 64);
+      if (sq_live && sq_x && sq_kc == 0) {
+        const int c = (int)tl.m0 + sq_r0;
 #pragma unroll
         for (int v = 0; v < V; ++v)
           if (c + v < a.N) a.db[(int64_t)tl.e * a.N + c + v] = dbs[v];
@@ -530,60 +644,76 @@ __global__ __launch_bounds__(256, 2) void k_expert_tile(ExpertArgs a) {
   }
 
   // ---- output
-  const bool v4 = ((cols | (int)a.out_stride) & 3) == 0 && (uintptr_t)a.out % (OUT16 ? 8 : 16) == 0;
-  const int64_t rows = PASS == kDw ? a.N : tl.cnt;
-  const float* bias = PASS == kForward && a.bias ? a.bias + (int64_t)tl.e * a.N : nullptr;
+  __syncthreads();                                 // every wave is past its reads of the buffers
+  if (biased && tid < kWR) bs[tid] = bias;
+  __syncthreads();
+  if (has_rows) {
+    char* stage = smem + wu * 32 * kRowB;
 #pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const int64_t r = tl.m0 + wm * 64 + 32 * i + l32;
-    if (r >= rows) continue;
-    const int64_t orow = PASS == kDw ? (int64_t)tl.e * a.N + r : tl.s0 + r;
-    const S* mrow = nullptr;
-    if constexpr (PASS == kDx) {
-      if (a.mask) {
-        const int64_t mr = placed_row(a.mask_order, a.k, a.mask_rows, tl.s0 + r);
-        mrow = (const S*)((const char*)a.mask + (mr < 0 ? 0 : mr) * a.mask_stride);
-      }
-    }
+    for (int i = 0; i < MI; ++i)
 #pragma unroll
-    for (int t = 0; t < 4; ++t)
+      for (int t0 = 0; t0 < NI; t0 += kTs) {
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const int c = n0 + wn * 128 + 32 * t + 8 * q + 4 * lh;
-        if (c >= cols) continue;
-        float f[4];
+        for (int t = t0; t < t0 + kTs; ++t)
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
-          f[u] = acc[i][t][4 * q + u];
-          if (c + u < cols) {
-            if (bias) f[u] += bias[c + u];
-            if (PASS == kForward && a.relu) f[u] = f[u] > 0.0f || f[u] != f[u] ? f[u] : 0.0f;
-            if constexpr (PASS == kDx && !mx) {
-              if (mrow && !(Op<S>::to_f32(mrow[c + u]) > 0.0f)) f[u] = 0.0f;
+          for (int q = 0; q < 4; ++q) {
+            float f[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) f[u] = acc[i][t][4 * q + u];
+            if (biased) {
+              const float4 c = *reinterpret_cast<const float4*>(bs + wn * 32 * NI + 32 * t + 8 * q + 4 * lh);
+              f[0] += c.x; f[1] += c.y; f[2] += c.z; f[3] += c.w;
+            }
+            if (PASS == kForward && a.relu) {
+#pragma unroll
+              for (int u = 0; u < 4; ++u) f[u] = f[u] < 0.0f ? 0.0f : f[u];   // (NaN stays)
+            }
+            char* row = stage + l32 * kRowB;
+            if constexpr (OUT16) {                 // chunk 4 t + q, half lh
+              const int ch = (4 * (t - t0) + q) ^ (l32 & (kCh - 1));
+              *reinterpret_cast<uint2*>(row + 16 * ch + 8 * lh) = make_uint2(bf16x2(f[0], f[1]), bf16x2(f[2], f[3]));
+            } else {
+              const int ch = (8 * (t - t0) + 2 * q + lh) ^ (l32 & (kCh - 1));
+              *reinterpret_cast<float4*>(row + 16 * ch) = make_float4(f[0], f[1], f[2], f[3]);
             }
           }
-        }
-        if constexpr (OUT16) {
-          uint16_t* o = (uint16_t*)a.out + orow * a.out_stride + c;
-          const uint2 p = make_uint2(bf16x2(f[0], f[1]), bf16x2(f[2], f[3]));
-          if (v4) {
-            *reinterpret_cast<uint2*>(o) = p;
-          } else {
-            o[0] = (uint16_t)p.x;
-            if (c + 1 < cols) o[1] = (uint16_t)(p.x >> 16);
-            if (c + 2 < cols) o[2] = (uint16_t)p.y;
-            if (c + 3 < cols) o[3] = (uint16_t)(p.y >> 16);
-          }
-        } else {
-          float* o = (float*)a.out + orow * a.out_stride + c;
-          if (v4) {
-            *reinterpret_cast<float4*>(o) = make_float4(f[0], f[1], f[2], f[3]);
-          } else {
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll
-            for (int u = 0; u < 4; ++u)
-              if (c + u < cols) o[u] = f[u];
+        for (int j = 0; j < kCh / 2; ++j) {        // 64 / kCh rows an instruction
+          const int rr = j * (64 / kCh) + lane / kCh, ch = lane % kCh;
+          uint4 u = *reinterpret_cast<const uint4*>(stage + rr * kRowB + 16 * (ch ^ (rr & (kCh - 1))));
+          const int64_t r = tl.m0 + wm * 32 * MI + 32 * i + rr;
+          const int c = n0 + wn * 32 * NI + 32 * t0 + ch * kEl;
+          if (r >= rows || c >= cols) continue;
+          if constexpr (PASS == kDx && !mx) {
+            if (a.mask) {
+              const int64_t mr = placed_row(a.mask_order, a.k, a.mask_rows, tl.s0 + r);
+              const char* mp = (const char*)a.mask + (mr < 0 ? 0 : mr) * a.mask_stride + (size_t)c * sizeof(S);
+              const uint4 mu = load_chunk<S>(mp, cols - c);
+              S me[V];
+              O oe[kEl];
+              static_assert(PASS != kDx || V == kEl, "dx has its input's type");
+              __builtin_memcpy(me, &mu, 16);
+              __builtin_memcpy(oe, &u, 16);
+#pragma unroll
+              for (int v = 0; v < kEl; ++v)
+                if (!(Op<S>::to_f32(me[v]) > 0.0f)) oe[v] = 0;
+              __builtin_memcpy(&u, oe, 16);
+            }
+          }
+          const int64_t orow = PASS == kDw ? (int64_t)tl.e * a.N + r : tl.s0 + r;
+          O* o = (O*)a.out + orow * a.out_stride + c;
+          if (whole) {
+            *reinterpret_cast<uint4*>(o) = u;
+          } else {
+            O oe[kEl];
+            __builtin_memcpy(oe, &u, 16);
+#pragma unroll
+            for (int v = 0; v < kEl; ++v)
+              if (c + v < cols) o[v] = oe[v];
           }
         }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
       }
   }
 }
@@ -602,20 +732,20 @@ __global__ __launch_bounds__(256) void k_expert_few(ExpertArgs a) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l16 = lane & 15, lk = lane >> 4;
   int e = (int)blockIdx.y;
   if (a.offsets) {                                   // the blockIdx.y-th expert with rows
-    int left = (int)blockIdx.y, found = -1;
-    for (int b = 0; b < a.E && found < 0; b += 64) {
-      int64_t s0, cnt = 0;
-      if (b + lane < a.E) segment(a, b + lane, s0, cnt);
-      uint64_t in = __ballot(cnt > 0);
-      const int n = __popcll(in);
-      if (left < n) {
-        for (; left > 0; --left) in &= in - 1;
-        found = b + __ffsll((unsigned long long)in) - 1;
-      }
-      left -= n;
+  int left = (int)blockIdx.y, found = -1;
+  for (int b = 0; b < a.E && found < 0; b += 64) {
+    int64_t s0, cnt = 0;
+    if (b + lane < a.E) segment(a, b + lane, s0, cnt);
+    uint64_t in = __ballot(cnt > 0);
+    const int n = __popcll(in);
+    if (left < n) {
+      for (; left > 0; --left) in &= in - 1;
+      found = b + __ffsll((unsigned long long)in) - 1;
     }
-    if (found < 0) return;
-    e = __builtin_amdgcn_readfirstlane(found);
+    left -= n;
+  }
+  if (found < 0) return;
+  e = __builtin_amdgcn_readfirstlane(found);
   }
   int64_t s0, cnt;
   segment(a, e, s0, cnt);
@@ -625,77 +755,113 @@ __global__ __launch_bounds__(256) void k_expert_few(ExpertArgs a) {
   const char* wrow = (const char*)a.w + e * a.w_e + (n < a.N ? n : 0) * a.w_n + 16 * lk;
   const char* wsrow = mx ? (const char*)a.ws + e * a.ws_e + (n < a.N ? n : 0) * a.ws_n + lk : nullptr;
   for (int64_t m0 = 0; m0 < cnt; m0 += 16) {
-    const int64_t i = m0 + l16;
-    const int64_t r = i < cnt ? source_row(a, s0, i) : -1;
-    const int64_t xe = a.offsets ? 0 : (int64_t)e;
-    const char* xrow = (const char*)a.x + xe * a.x_e + (r < 0 ? 0 : r) * a.x_stride + 16 * lk;
-    const char* xsrow = mx ? (const char*)a.xs + xe * a.xs_e + (r < 0 ? 0 : r) * a.xs_stride + lk : nullptr;
-    f32x4_t acc = {0.0f, 0.0f, 0.0f, 0.0f};
-    auto load = [&](const char* p, bool have, int st) -> uint4 {
-      const int left = bytes - st * 64 - 16 * lk;
-      if constexpr (VEC || mx) {
-        return have && left > 0 ? *reinterpret_cast<const uint4*>(p + st * 64) : make_uint4(0, 0, 0, 0);
-      } else {
-        return load_chunk<S>(p + st * 64, have ? left / (int)sizeof(S) : 0, false);
-      }
-    };
-    constexpr int U = 8;
-    for (int b = st0; b < st1; b += U) {
-      uint4 fw[U], fx[U];
-      uint32_t sw[U], sx[U];
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const bool in = b + u < st1;
-        fw[u] = load(wrow, in && n < a.N, b + u);
-        fx[u] = load(xrow, in && r >= 0, b + u);
-        sw[u] = sx[u] = 0;
-        if constexpr (mx) {
-          if (in && n < a.N) sw[u] = (uint8_t)wsrow[(b + u) * 4];
-          if (in && r >= 0) sx[u] = (uint8_t)xsrow[(b + u) * 4];
-        }
-      }
-#pragma unroll
-      for (int u = 0; u < U; ++u) acc = M::mma16(fw[u], fx[u], acc, sw[u], sx[u]);
+  const int64_t i = m0 + l16;
+  const int64_t r = i < cnt ? source_row(a, s0, i) : -1;
+  const int64_t xe = a.offsets ? 0 : (int64_t)e;
+  const char* xrow = (const char*)a.x + xe * a.x_e + (r < 0 ? 0 : r) * a.x_stride + 16 * lk;
+  const char* xsrow = mx ? (const char*)a.xs + xe * a.xs_e + (r < 0 ? 0 : r) * a.xs_stride + lk : nullptr;
+  f32x4_t acc = {0.0f, 0.0f, 0.0f, 0.0f};
+  auto load = [&](const char* p, bool have, int st) -> uint4 {
+    const int left = bytes - st * 64 - 16 * lk;
+    if constexpr (VEC || mx) {
+      return have && left > 0 ? *reinterpret_cast<const uint4*>(p + st * 64) : make_uint4(0, 0, 0, 0);
+    } else {
+      return load_chunk<S>(p + st * 64, have ? left / (int)sizeof(S) : 0);
     }
-    __syncthreads();                                 // the last tile's sums have been read
-    part[wave][lane] = acc;
-    __syncthreads();
-    if (wave == 0 && r >= 0) {                       // lane: row l16, columns n0 + 4 lk + 0 .. 3
-      const f32x4_t sum = part[0][lane] + part[1][lane] + part[2][lane] + part[3][lane];
+  };
+  constexpr int U = 8;
+  for (int b = st0; b < st1; b += U) {
+    uint4 fw[U], fx[U];
+    uint32_t sw[U], sx[U];
 #pragma unroll
-      for (int u = 0; u < 4; ++u) {
-        const int c = n0 + 4 * lk + u;
-        if (c >= a.N) continue;
-        float f = sum[u];
-        if (a.bias) f += a.bias[(int64_t)e * a.N + c];
-        if (a.relu) f = f > 0.0f || f != f ? f : 0.0f;
-        const int64_t at = (s0 + i) * a.out_stride + c;
-        if constexpr (OUT16) ((uint16_t*)a.out)[at] = f32_to_bf16_bits(f);
-        else ((float*)a.out)[at] = f;
+    for (int u = 0; u < U; ++u) {
+      const bool in = b + u < st1;
+      fw[u] = load(wrow, in && n < a.N, b + u);
+      fx[u] = load(xrow, in && r >= 0, b + u);
+      sw[u] = sx[u] = 0;
+      if constexpr (mx) {
+        if (in && n < a.N) sw[u] = (uint8_t)wsrow[(b + u) * 4];
+        if (in && r >= 0) sx[u] = (uint8_t)xsrow[(b + u) * 4];
       }
     }
+#pragma unroll
+    for (int u = 0; u < U; ++u) acc = M::mma16(fw[u], fx[u], acc, sw[u], sx[u]);
+  }
+  __syncthreads();                                 // the last tile's sums have been read
+  part[wave][lane] = acc;
+  __syncthreads();
+  if (wave == 0 && r >= 0) {                       // lane: row l16, columns n0 + 4 lk + 0 .. 3
+    const f32x4_t sum = part[0][lane] + part[1][lane] + part[2][lane] + part[3][lane];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int c = n0 + 4 * lk + u;
+      if (c >= a.N) continue;
+      float f = sum[u];
+      if (a.bias) f += a.bias[(int64_t)e * a.N + c];
+      if (a.relu) f = f > 0.0f || f != f ? f : 0.0f;
+      const int64_t at = (s0 + i) * a.out_stride + c;
+      if constexpr (OUT16) ((uint16_t*)a.out)[at] = f32_to_bf16_bits(f);
+      else ((float*)a.out)[at] = f;
+    }
+  }
   }
 }
 
 namespace {
 
-template <ExpertType TY, Pass PASS, Load XL, Load WL, bool OUT16>
+template <typename SH, ExpertType TY, Pass PASS, Load XL, Load WL, bool OUT16>
 hipError_t tile_go(const ExpertArgs& a, int64_t tiles, hipStream_t s) {
-  constexpr size_t lds = kBufs * (size_t)(kXBytes + kWBytes + (TY == kTypeMx4 ? kScaleBytes : 0));
-  auto* fn = k_expert_tile<TY, PASS, XL, WL, OUT16>;
-  hipError_t err = hipFuncSetAttribute(reinterpret_cast<const void*>(fn), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
-  if (err != hipSuccess) return err;
-  tiles = (tiles + 7) / 8 * 8;
+  constexpr size_t lds =
+      2 * (size_t)(SH::kXBytes + SH::kWBytes + (TY == kTypeMx4 ? SH::kScaleBytes : 0)) + SH::kWR * 4;
+  static_assert(lds * SH::WGS <= 160 * 1024, "workgroups of a CU share its LDS");
+  auto* fn = k_expert_tile<SH, TY, PASS, XL, WL, OUT16>;
+  if (lds > 64 * 1024) {
+    const hipError_t err = hipFuncSetAttribute(reinterpret_cast<const void*>(fn),
+                                               hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+    if (err != hipSuccess) return err;
+  }
   if (tiles > 0x7ffffff8) return hipErrorInvalidValue;
-  fn<<<(unsigned)tiles, 256, lds, s>>>(a);
+  fn<<<(unsigned)((tiles + 7) / 8 * 8), SH::kThreads, lds, s>>>(a);
   return hipGetLastError();
 }
 
 // most tiles that the segments can have: one part tile for each expert with rows
-int64_t forward_tiles(const ExpertArgs& a) {
-  const int64_t nt = (a.N + kWR - 1) / kWR;
-  if (!a.offsets) return (a.M + kXR - 1) / kXR * a.E * nt;
-  return (a.S / kXR + (a.S < a.E ? a.S : a.E)) * nt;
+template <typename SH>
+int64_t most_tiles(const ExpertArgs& a, Pass pass) {
+  const int64_t nt = ((pass == kDw ? a.K : a.N) + SH::kWR - 1) / SH::kWR;
+  if (pass == kDw) return (int64_t)a.E * ((a.N + SH::kXR - 1) / SH::kXR) * nt;
+  if (!a.offsets) return (a.M + SH::kXR - 1) / SH::kXR * a.E * nt;
+  return (a.S / SH::kXR + (a.S < a.E ? a.S : a.E)) * nt;
+}
+
+// Time of the tiles on 256 CUs in units of a 64 x 64 tile's share of a busy CU:
+// rounds of tiles times what a tile takes, `cost` for each 64 x 64 of it, and
+// no less than `least` for a round.  Expected tiles count half a part tile for
+// each expert with rows.
+template <typename SH>
+int64_t tile_time(const ExpertArgs& a, Pass pass, int cost, int least) {
+  int64_t n = most_tiles<SH>(a, pass);
+  if (pass != kDw && a.offsets) n -= (a.S < a.E ? a.S : a.E) * ((a.N + SH::kWR - 1) / SH::kWR) / 2;
+  const int64_t area = SH::kXR / 64 * (SH::kWR / 64), t = (n + 255) / 256 * area * cost;
+  return t > least * area ? t : least * area;
+}
+
+template <ExpertType TY, Pass PASS, Load XL, Load WL, bool OUT16>
+hipError_t tile_shape(const ExpertArgs& a, hipStream_t s) {
+  typedef typename Shapes<TY>::Wide Wide;
+  typedef typename Shapes<TY>::Mid Mid;
+  typedef typename Shapes<TY>::Small Small;
+  //TUNE
+  { const char* f = getenv("GEVO_SHAPE"); if (f && f[0]) {
+    if (f[0]=='0') return tile_go<Wide, TY, PASS, XL, WL, OUT16>(a, most_tiles<Wide>(a, PASS), s);
+    if (f[0]=='1') return tile_go<Mid, TY, PASS, XL, WL, OUT16>(a, most_tiles<Mid>(a, PASS), s);
+    return tile_go<Small, TY, PASS, XL, WL, OUT16>(a, most_tiles<Small>(a, PASS), s); } }
+  //TUNE
+  const int64_t w = tile_time<Wide>(a, PASS, 10, 10), m = tile_time<Mid>(a, PASS, 13, 20),
+                n = tile_time<Small>(a, PASS, 20, 40);
+  if (w <= m && w <= n) return tile_go<Wide, TY, PASS, XL, WL, OUT16>(a, most_tiles<Wide>(a, PASS), s);
+  if (m <= n) return tile_go<Mid, TY, PASS, XL, WL, OUT16>(a, most_tiles<Mid>(a, PASS), s);
+  return tile_go<Small, TY, PASS, XL, WL, OUT16>(a, most_tiles<Small>(a, PASS), s);
 }
 
 bool aligned16(const void* p, int64_t a, int64_t b, int64_t c) {
@@ -714,19 +880,17 @@ hipError_t forward_out(const ExpertArgs& a, hipStream_t s) {
     else k_expert_few<TY, false, OUT16><<<grid, 256, 0, s>>>(a);
     return hipGetLastError();
   }
-  const int64_t tiles = forward_tiles(a);
-  if constexpr (TY == kTypeMx4) return tile_go<TY, kForward, kDma, kDma, OUT16>(a, tiles, s);
-  else if (vec) return tile_go<TY, kForward, kDma, kDma, OUT16>(a, tiles, s);
-  else return tile_go<TY, kForward, kGuarded, kGuarded, OUT16>(a, tiles, s);
+  if constexpr (TY == kTypeMx4) return tile_shape<TY, kForward, kDma, kDma, OUT16>(a, s);
+  else if (vec) return tile_shape<TY, kForward, kDma, kDma, OUT16>(a, s);
+  else return tile_shape<TY, kForward, kGuarded, kGuarded, OUT16>(a, s);
 }
 
 template <ExpertType TY>
 hipError_t dx_go(const ExpertArgs& a, hipStream_t s) {
   constexpr bool o16 = TY == kTypeBf16;
-  const int64_t tiles = forward_tiles(a);
   if (aligned16(a.x, a.x_stride, 0, a.K * (int64_t)sizeof(typename Mm<TY>::S)))
-    return tile_go<TY, kDx, kDma, kTransposed, o16>(a, tiles, s);
-  return tile_go<TY, kDx, kGuarded, kTransposed, o16>(a, tiles, s);
+    return tile_shape<TY, kDx, kDma, kTransposed, o16>(a, s);
+  return tile_shape<TY, kDx, kGuarded, kTransposed, o16>(a, s);
 }
 
 }  // namespace
@@ -744,9 +908,8 @@ hipError_t launch_expert_dx(const ExpertArgs& a, ExpertType type, hipStream_t s)
 }
 
 hipError_t launch_expert_dw(const ExpertArgs& a, ExpertType type, hipStream_t s) {
-  const int64_t tiles = (int64_t)a.E * ((a.N + kXR - 1) / kXR) * ((a.K + kWR - 1) / kWR);
-  if (type == kTypeF32) return tile_go<kTypeF32, kDw, kTransposed, kTransposed, false>(a, tiles, s);
-  return tile_go<kTypeBf16, kDw, kTransposed, kTransposed, false>(a, tiles, s);
+  if (type == kTypeF32) return tile_shape<kTypeF32, kDw, kTransposed, kTransposed, false>(a, s);
+  return tile_shape<kTypeBf16, kDw, kTransposed, kTransposed, false>(a, s);
 }
 
 }  // namespace gevo

@@ -162,7 +162,7 @@ gevo_status gevo_route_plan(int64_t slots, uint32_t E, const int32_t* ids, void*
   if (st != GEVO_OK) return st;
   if (!ptr_ok(offsets, 4)) return GEVO_E_ARG;
   if (slots > 0 && (!ptr_ok(ids, 4) || !ptr_ok(order, 4) || !ptr_ok(pos, 4))) return GEVO_E_ARG;
-  if (!ptr_ok(ws, 4) || ws_bytes < need) return GEVO_E_WORKSPACE;
+  if (need > 0 && (!ptr_ok(ws, 4) || ws_bytes < need)) return GEVO_E_WORKSPACE;
   return done(launch_route_plan(ids, slots, (int)E, static_cast<uint32_t*>(ws), order, pos, offsets,
                                 static_cast<hipStream_t>(stream)));
 }

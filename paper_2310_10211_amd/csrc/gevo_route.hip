@@ -495,7 +495,7 @@ __global__ __launch_bounds__(256) void k_plan_place(const int32_t* ids, int64_t 
 }
 
 size_t plan_workspace_bytes(int64_t slots, int E) {
-  if (slots <= kPlanChunk) return 256;
+  if (slots <= kPlanChunk) return 0;
   const size_t chunks = (size_t)((slots + kPlanChunk - 1) / kPlanChunk);
   return ((chunks + 1) * (size_t)E * 4 + 255) / 256 * 256;
 }

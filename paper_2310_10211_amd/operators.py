@@ -21,6 +21,7 @@ and backward: expert_combine_backward, expert_backward, route_backward.
 from __future__ import annotations
 
 import ctypes
+import functools
 
 import torch
 
@@ -53,52 +54,75 @@ class Mx4Config(ctypes.Structure):
                 ("a_each", _u32), ("k", _u32), ("sorted_rows", _u32), ("relu", _u32)]
 
 
-def _need(ok, what):
-    if not ok:
-        raise GevoError(what)
-
-
 def _rows(t, name, dims=2):
     """t with dims dimensions, of a type that the kernels take, its last one contiguous."""
-    _need(isinstance(t, torch.Tensor) and t.is_cuda, f"{name}: a tensor on the GPU")
-    _need(t.dtype in DTYPES, f"{name}: float32 or bfloat16, not {t.dtype}")
-    _need(t.dim() == dims, f"{name}: {dims} dimensions, not {t.dim()}")
+    if not (isinstance(t, torch.Tensor) and t.is_cuda):
+        raise GevoError(f"{name}: a tensor on the GPU")
+    if t.dtype not in DTYPES:
+        raise GevoError(f"{name}: float32 or bfloat16, not {t.dtype}")
+    if t.dim() != dims:
+        raise GevoError(f"{name}: {dims} dimensions, not {t.dim()}")
     return t if t.shape[-1] <= 1 or t.stride(-1) == 1 else t.contiguous()
 
 
 def _flat(t, name, dtype, shape, device):
     """t as a contiguous tensor of one type and shape."""
-    _need(isinstance(t, torch.Tensor) and t.device == device, f"{name}: a tensor on {device}")
-    _need(t.dtype == dtype and tuple(t.shape) == tuple(shape), f"{name}: {dtype} of shape {tuple(shape)}, not "
-          f"{t.dtype} of {tuple(t.shape)}")
+    if not (isinstance(t, torch.Tensor) and t.device == device):
+        raise GevoError(f"{name}: a tensor on {device}")
+    if t.dtype != dtype or t.shape != shape:
+        raise GevoError(f"{name}: {dtype} of shape {tuple(shape)}, not {t.dtype} of {tuple(t.shape)}")
     return t if t.is_contiguous() else t.contiguous()
 
 
-def _stride(t, dim=0):
-    """Elements between t's rows; at least a row's length where there is one row or none."""
-    return max(t.stride(dim), t.shape[-1]) if t.shape[dim] > 1 else t.shape[-1]
+def _stride(t):
+    """Elements between t's rows; a row's length where there is one row or none."""
+    return t.stride(0) if t.shape[0] > 1 else t.shape[-1]
 
 
 def _out_dtype(dtype, default):
-    dtype = default if dtype is None else dtype
-    _need(dtype in DTYPES, f"out_dtype: float32 or bfloat16, not {dtype}")
+    if dtype is None:
+        return default
+    if dtype not in DTYPES:
+        raise GevoError(f"out_dtype: float32 or bfloat16, not {dtype}")
     return dtype
+
+
+# (the pointer of torch's current stream, without the object around it)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+    lambda index: torch.cuda.current_stream(index).cuda_stream)
 
 
 def _call(name, device, *args):
     """The library's call `name` on the device's current stream."""
-    fn = getattr(lib(), name)
-    if device.index == torch.cuda.current_device():
-        rc = fn(*args, torch.cuda.current_stream(device).cuda_stream)
+    index = device.index
+    if index == torch.cuda.current_device():
+        rc = getattr(lib(), name)(*args, _raw_stream(index))
     else:
-        with torch.cuda.device(device):
-            rc = fn(*args, torch.cuda.current_stream(device).cuda_stream)
+        with torch.cuda.device(index):
+            rc = getattr(lib(), name)(*args, _raw_stream(index))
     if rc:
         _check(rc, name)
 
 
 def _ptr(t):
     return None if t is None else t.data_ptr()
+
+
+# The configurations of calls, by their values: a program repeats a few, and the
+# library reads them during the call alone.
+def _config(cls):
+    return functools.lru_cache(maxsize=1024)(lambda *values: ctypes.byref(cls(GEVO_ABI_VERSION, *values)))
+
+
+_route_cfg, _expert_cfg = _config(RouteConfig), _config(ExpertConfig)
+_combine_cfg, _mx4_cfg = _config(CombineConfig), _config(Mx4Config)
+
+
+@functools.lru_cache(maxsize=1024)
+def _plan_bytes(slots, n_experts):
+    nbytes = ctypes.c_size_t()
+    _check(lib().gevo_route_plan_bytes(slots, n_experts, ctypes.byref(nbytes)), "gevo_route_plan_bytes")
+    return nbytes.value
 
 
 class RoutePlan:
@@ -108,9 +132,10 @@ class RoutePlan:
     __slots__ = ("order", "pos", "offsets")
 
     def __init__(self, order, pos, offsets):
-        _need(isinstance(pos, torch.Tensor) and pos.is_cuda and pos.dim() == 2, "pos: a tensor [T][k] on the GPU")
-        _need(isinstance(offsets, torch.Tensor) and offsets.dim() == 1 and offsets.numel() >= 2,
-              "offsets: a tensor [E + 1]")
+        if not (isinstance(pos, torch.Tensor) and pos.is_cuda and pos.dim() == 2):
+            raise GevoError("pos: a tensor [T][k] on the GPU")
+        if not (isinstance(offsets, torch.Tensor) and offsets.dim() == 1 and offsets.numel() >= 2):
+            raise GevoError("offsets: a tensor [E + 1]")
         self.pos = _flat(pos, "pos", torch.int32, pos.shape, pos.device)
         self.order = _flat(order, "order", torch.int32, (pos.numel(),), pos.device)
         self.offsets = _flat(offsets, "offsets", torch.int32, offsets.shape, pos.device)
@@ -120,12 +145,20 @@ class RoutePlan:
         return self.offsets.numel() - 1
 
 
+def _plan_of(plan, device):
+    if not (isinstance(plan, RoutePlan) and plan.pos.device == device):
+        raise GevoError(f"plan: a RoutePlan on {device}")
+    return plan
+
+
 def _route_config(logits, k, score, groups, top_groups, group_top, renorm, scale):
-    _need(score in SCORES, f"score: one of {sorted(SCORES)}, not {score!r}")
+    if score not in SCORES:
+        raise GevoError(f"score: one of {sorted(SCORES)}, not {score!r}")
+    if min(k, groups, top_groups, group_top) < 1:
+        raise GevoError("top_k, groups, top_groups and group_top: at least 1")
     T, E = logits.shape
-    _need(min(k, groups, top_groups, group_top) >= 1, "top_k, groups, top_groups and group_top: at least 1")
-    return RouteConfig(GEVO_ABI_VERSION, E, k, T, DTYPES[logits.dtype], SCORES[score], _stride(logits), groups,
-                       top_groups, group_top, 1 if renorm else 0, scale)
+    return _route_cfg(E, k, T, DTYPES[logits.dtype], SCORES[score], _stride(logits) if T > 1 else E, groups,
+                      top_groups, group_top, 1 if renorm else 0, scale)
 
 
 def route(logits, top_k, *, score="softmax", bias=None, groups=1, top_groups=1, group_top=1, renorm=True, scale=1.0):
@@ -135,10 +168,12 @@ def route(logits, top_k, *, score="softmax", bias=None, groups=1, top_groups=1, 
     dev = logits.device
     if bias is not None:
         bias = _flat(bias, "bias", torch.float32, logits.shape[1:], dev)
+    if logits.shape[0] > 1 and logits.stride(0) < logits.shape[1]:
+        logits = logits.contiguous()                 # rows that overlap (expanded)
     cfg = _route_config(logits, top_k, score, groups, top_groups, group_top, renorm, scale)
     weights = torch.empty((logits.shape[0], top_k), dtype=torch.float32, device=dev)
     ids = torch.empty((logits.shape[0], top_k), dtype=torch.int32, device=dev)
-    _call("gevo_route", dev, ctypes.byref(cfg), _ptr(logits), _ptr(bias), _ptr(weights), _ptr(ids))
+    _call("gevo_route", dev, cfg, logits.data_ptr(), _ptr(bias), weights.data_ptr(), ids.data_ptr())
     return weights, ids
 
 
@@ -147,51 +182,59 @@ def route_backward(logits, ids, dweights, *, score="softmax", renorm=True, scale
     with gradient dweights [T][k] and choice ids (gevo_route_backward)."""
     logits = _rows(logits, "logits")
     dev = logits.device
-    _need(isinstance(ids, torch.Tensor) and ids.dim() == 2, "ids: a tensor [T][k]")
+    if not (isinstance(ids, torch.Tensor) and ids.dim() == 2):
+        raise GevoError("ids: a tensor [T][k]")
     shape = (logits.shape[0], ids.shape[1])
     ids = _flat(ids, "ids", torch.int32, shape, dev)
     dweights = _flat(dweights, "dweights", torch.float32, shape, dev)
+    if shape[0] > 1 and logits.stride(0) < logits.shape[1]:
+        logits = logits.contiguous()
     cfg = _route_config(logits, shape[1], score, 1, 1, 1, renorm, scale)
     out = torch.empty(logits.shape, dtype=logits.dtype, device=dev)
-    _call("gevo_route_backward", dev, ctypes.byref(cfg), _ptr(logits), _ptr(ids), _ptr(dweights), _ptr(out))
+    _call("gevo_route_backward", dev, cfg, logits.data_ptr(), ids.data_ptr(), dweights.data_ptr(), out.data_ptr())
     return out
 
 
 def route_plan(ids, n_experts) -> RoutePlan:
     """The slots of ids [T][k] sorted by expert (gevo_route_plan)."""
-    _need(isinstance(ids, torch.Tensor) and ids.is_cuda and ids.dim() == 2, "ids: a tensor [T][k] on the GPU")
-    _need(n_experts >= 1, "n_experts: at least 1")
+    if not (isinstance(ids, torch.Tensor) and ids.is_cuda and ids.dim() == 2):
+        raise GevoError("ids: a tensor [T][k] on the GPU")
+    if n_experts < 1:
+        raise GevoError("n_experts: at least 1")
     dev = ids.device
     ids = _flat(ids, "ids", torch.int32, ids.shape, dev)
     n = ids.numel()
-    nbytes = ctypes.c_size_t()
-    _check(lib().gevo_route_plan_bytes(n, n_experts, ctypes.byref(nbytes)), "gevo_route_plan_bytes")
-    ws = torch.empty(nbytes.value, dtype=torch.uint8, device=dev)
-    order = torch.empty(n, dtype=torch.int32, device=dev)
-    pos = torch.empty(ids.shape, dtype=torch.int32, device=dev)
-    offsets = torch.empty(n_experts + 1, dtype=torch.int32, device=dev)
-    _call("gevo_route_plan", dev, n, n_experts, _ptr(ids), _ptr(ws), nbytes.value, _ptr(order), _ptr(pos),
-          _ptr(offsets))
-    return RoutePlan(order, pos, offsets)
+    nbytes = _plan_bytes(n, n_experts)
+    ws = torch.empty(nbytes, dtype=torch.uint8, device=dev) if nbytes else None
+    plan = RoutePlan.__new__(RoutePlan)
+    plan.order = torch.empty(n, dtype=torch.int32, device=dev)
+    plan.pos = torch.empty(ids.shape, dtype=torch.int32, device=dev)
+    plan.offsets = torch.empty(n_experts + 1, dtype=torch.int32, device=dev)
+    _call("gevo_route_plan", dev, n, n_experts, ids.data_ptr(), _ptr(ws), nbytes, plan.order.data_ptr(),
+          plan.pos.data_ptr(), plan.offsets.data_ptr())
+    return plan
 
 
 def _expert_setup(x, w, plan, sorted_rows, y_stride, relu, out_dtype):
     x, w = _rows(x, "x"), _rows(w, "w", 3)
     dev = x.device
-    _need(isinstance(plan, RoutePlan) and plan.pos.device == dev, f"plan: a RoutePlan on {dev}")
-    _need(w.device == dev and w.dtype == x.dtype, f"w: {x.dtype} on {dev}")
+    _plan_of(plan, dev)
+    if w.device != dev or w.dtype != x.dtype:
+        raise GevoError(f"w: {x.dtype} on {dev}")
     (T, k), (E, N, K) = plan.pos.shape, w.shape
-    _need(E == plan.n_experts, f"w: {plan.n_experts} experts as the plan has, not {E}")
+    if E != plan.n_experts:
+        raise GevoError(f"w: {plan.n_experts} experts as the plan has, not {E}")
     rows = T * k if sorted_rows else T
-    _need(tuple(x.shape) == (rows, K), f"x: shape {(rows, K)}, not {tuple(x.shape)}")
+    if x.shape != (rows, K):
+        raise GevoError(f"x: shape {(rows, K)}, not {tuple(x.shape)}")
     if (N > 1 and w.stride(1) < K) or (E > 1 and w.stride(0) < (N - 1) * w.stride(1) + K):
         w = w.contiguous()                           # overlapping or transposed matrices
     if rows > 1 and x.stride(0) < K:
         x = x.contiguous()
     wn = w.stride(1) if N > 1 else K
     we = w.stride(0) if E > 1 else (N - 1) * wn + K
-    cfg = ExpertConfig(GEVO_ABI_VERSION, DTYPES[x.dtype], DTYPES[out_dtype or x.dtype], E, k, N, K, T, _stride(x), we,
-                       wn, y_stride or N, 1 if sorted_rows else 0, 1 if relu else 0)
+    cfg = _expert_cfg(DTYPES[x.dtype], DTYPES[out_dtype], E, k, N, K, T, _stride(x), we, wn, y_stride or N,
+                      1 if sorted_rows else 0, 1 if relu else 0)
     return x, w, cfg, dev
 
 
@@ -200,13 +243,13 @@ def expert_forward(x, w, plan, bias=None, *, relu=False, sorted_rows=False, out_
     [E][N][K], bias [E][N] float32 (gevo_expert_forward).  x is [T][K], or with
     sorted_rows the sorted rows of a layer before, [T k][K].  Rows of slots
     without an expert (from plan.offsets[-1] on) hold nothing."""
-    out_dtype = _out_dtype(out_dtype, x.dtype if isinstance(x, torch.Tensor) else None)
+    out_dtype = _out_dtype(out_dtype, _rows(x, "x").dtype)
     x, w, cfg, dev = _expert_setup(x, w, plan, sorted_rows, 0, relu, out_dtype)
     if bias is not None:
         bias = _flat(bias, "bias", torch.float32, w.shape[:2], dev)
     out = torch.empty((plan.pos.numel(), w.shape[1]), dtype=out_dtype, device=dev)
-    _call("gevo_expert_forward", dev, ctypes.byref(cfg), _ptr(x), _ptr(w), _ptr(bias), _ptr(plan.order),
-          _ptr(plan.offsets), _ptr(out))
+    _call("gevo_expert_forward", dev, cfg, x.data_ptr(), w.data_ptr(), _ptr(bias), plan.order.data_ptr(),
+          plan.offsets.data_ptr(), out.data_ptr())
     return out
 
 
@@ -219,13 +262,13 @@ def expert_backward(dy, x, w, plan, *, sorted_rows=False, relu_input=False, need
     n = plan.pos.numel() if isinstance(plan, RoutePlan) else 0
     if n > 1 and dy.stride(0) < dy.shape[1]:
         dy = dy.contiguous()
-    x, w, cfg, dev = _expert_setup(x, w, plan, sorted_rows, _stride(dy), relu_input, None)
-    _need(dy.dtype == x.dtype and dy.device == dev and tuple(dy.shape) == (n, w.shape[1]),
-          f"dy: {x.dtype} of shape {(n, w.shape[1])} on {dev}, not {dy.dtype} of {tuple(dy.shape)}")
+    x, w, cfg, dev = _expert_setup(x, w, plan, sorted_rows, _stride(dy), relu_input, dy.dtype)
+    if dy.dtype != x.dtype or dy.device != dev or dy.shape != (n, w.shape[1]):
+        raise GevoError(f"dy: {x.dtype} of shape {(n, w.shape[1])} on {dev}, not {dy.dtype} of {tuple(dy.shape)}")
     dx = torch.empty((n, w.shape[2]), dtype=x.dtype, device=dev) if need_dx else None
     dw = torch.empty(w.shape, dtype=torch.float32, device=dev) if need_dw else None
     db = torch.empty(w.shape[:2], dtype=torch.float32, device=dev) if need_dw else None
-    _call("gevo_expert_backward", dev, ctypes.byref(cfg), _ptr(dy), _ptr(x), _ptr(w), _ptr(plan.order),
+    _call("gevo_expert_backward", dev, cfg, _ptr(dy), _ptr(x), _ptr(w), _ptr(plan.order),
           _ptr(plan.offsets), _ptr(dx), _ptr(dw), _ptr(db))
     return dx, dw, db
 
@@ -233,9 +276,11 @@ def expert_backward(dy, x, w, plan, *, sorted_rows=False, relu_input=False, need
 def _combine_setup(rows, plan, weights):
     rows = _rows(rows, "rows")
     dev = rows.device
-    _need(isinstance(plan, RoutePlan) and plan.pos.device == dev, f"plan: a RoutePlan on {dev}")
-    _need(rows.shape[0] == plan.pos.numel(), f"rows: {plan.pos.numel()} of them, not {rows.shape[0]}")
-    if rows.shape[0] > 1 and rows.stride(0) < rows.shape[1]:
+    _plan_of(plan, dev)
+    n = plan.pos.numel()
+    if rows.shape[0] != n:
+        raise GevoError(f"rows: {n} of them, not {rows.shape[0]}")
+    if n > 1 and rows.stride(0) < rows.shape[1]:
         rows = rows.contiguous()
     if weights is not None:
         weights = _flat(weights, "weights", torch.float32, plan.pos.shape, dev)
@@ -248,9 +293,9 @@ def expert_combine(rows, plan, weights=None, *, out_dtype=None):
     rows, weights, dev = _combine_setup(rows, plan, weights)
     out_dtype = _out_dtype(out_dtype, rows.dtype)
     (T, k), N = plan.pos.shape, rows.shape[1]
-    cfg = CombineConfig(GEVO_ABI_VERSION, DTYPES[rows.dtype], DTYPES[out_dtype], k, N, T, _stride(rows), N)
+    cfg = _combine_cfg(DTYPES[rows.dtype], DTYPES[out_dtype], k, N, T, _stride(rows), N)
     y = torch.empty((T, N), dtype=out_dtype, device=dev)
-    _call("gevo_expert_combine", dev, ctypes.byref(cfg), _ptr(rows), _ptr(plan.pos), _ptr(weights), _ptr(y))
+    _call("gevo_expert_combine", dev, cfg, rows.data_ptr(), plan.pos.data_ptr(), _ptr(weights), y.data_ptr())
     return y
 
 
@@ -260,17 +305,16 @@ def expert_combine_backward(dy, rows, plan, weights=None):
     rows, weights, dev = _combine_setup(rows, plan, weights)
     dy = _rows(dy, "dy")
     (T, k), N = plan.pos.shape, rows.shape[1]
-    _need(dy.dtype == rows.dtype and dy.device == dev and tuple(dy.shape) == (T, N),
-          f"dy: {rows.dtype} of shape {(T, N)} on {dev}, not {dy.dtype} of {tuple(dy.shape)}")
-    if T > 1 and 0 < dy.stride(0) < N:
+    if dy.dtype != rows.dtype or dy.device != dev or dy.shape != (T, N):
+        raise GevoError(f"dy: {rows.dtype} of shape {(T, N)} on {dev}, not {dy.dtype} of {tuple(dy.shape)}")
+    if T > 1 and dy.stride(0) < N:
         dy = dy.contiguous()
-    if T > 1 and dy.stride(0) == 0:                  # one gradient for every row (expanded)
-        dy = dy.contiguous()
-    cfg = CombineConfig(GEVO_ABI_VERSION, DTYPES[rows.dtype], DTYPES[rows.dtype], k, N, T, _stride(rows), _stride(dy))
+    dtype = DTYPES[rows.dtype]
+    cfg = _combine_cfg(dtype, dtype, k, N, T, _stride(rows), _stride(dy))
     drows = torch.empty((T * k, N), dtype=rows.dtype, device=dev)
     dweights = torch.empty((T, k), dtype=torch.float32, device=dev)
-    _call("gevo_expert_combine_backward", dev, ctypes.byref(cfg), _ptr(dy), _ptr(rows), _ptr(plan.pos),
-          _ptr(weights), _ptr(drows), _ptr(dweights))
+    _call("gevo_expert_combine_backward", dev, cfg, dy.data_ptr(), rows.data_ptr(), plan.pos.data_ptr(),
+          _ptr(weights), drows.data_ptr(), dweights.data_ptr())
     return drows, dweights
 
 
@@ -282,10 +326,11 @@ class Mx4:
     __slots__ = ("codes", "scales", "k")
 
     def __init__(self, codes, scales, k):
+        if not (k >= 1 and isinstance(codes, torch.Tensor) and codes.is_cuda and codes.dim() >= 2):
+            raise GevoError("codes: a tensor [..., rows, Kp / 2] on the GPU")
         kp = (k + 127) // 128 * 128
-        _need(k >= 1 and isinstance(codes, torch.Tensor) and codes.is_cuda and codes.dim() >= 2,
-              "codes: a tensor [..., rows, Kp / 2] on the GPU")
-        _need(codes.shape[-1] == kp // 2, f"codes: rows of {kp // 2} bytes for {k} values, not {codes.shape[-1]}")
+        if codes.shape[-1] != kp // 2:
+            raise GevoError(f"codes: rows of {kp // 2} bytes for {k} values, not {codes.shape[-1]}")
         self.codes = _flat(codes, "codes", torch.uint8, codes.shape, codes.device)
         self.scales = _flat(scales, "scales", torch.uint8, (*codes.shape[:-1], kp // 32), codes.device)
         self.k = k
@@ -297,28 +342,32 @@ class Mx4:
     def dequantize(self, dtype=torch.float32):
         """The values as a tensor of self.shape (gevo_mx4_dequantize)."""
         dtype = _out_dtype(dtype, torch.float32)
-        out = torch.empty(self.shape, dtype=dtype, device=self.codes.device)
-        _call("gevo_mx4_dequantize", self.codes.device, DTYPES[dtype], out.numel() // self.k, self.k,
-              _ptr(self.codes), _ptr(self.scales), _ptr(out), self.k)
+        k, dev = self.k, self.codes.device
+        out = torch.empty(self.shape, dtype=dtype, device=dev)
+        _call("gevo_mx4_dequantize", dev, DTYPES[dtype], out.numel() // k, k, self.codes.data_ptr(),
+              self.scales.data_ptr(), out.data_ptr(), k)
         return out
 
 
 def mx4_quantize(x) -> Mx4:
     """The rows of x [..., rows, K] in 4 bits, 32 values of a row to a scale
     (gevo_mx4_quantize)."""
-    _need(isinstance(x, torch.Tensor) and x.is_cuda and x.dim() >= 2 and x.shape[-1] >= 1,
-          "x: a tensor [..., rows, K] on the GPU")
-    _need(x.dtype in DTYPES, f"x: float32 or bfloat16, not {x.dtype}")
+    if not (isinstance(x, torch.Tensor) and x.is_cuda and x.dim() >= 2 and x.shape[-1] >= 1):
+        raise GevoError("x: a tensor [..., rows, K] on the GPU")
+    if x.dtype not in DTYPES:
+        raise GevoError(f"x: float32 or bfloat16, not {x.dtype}")
     k = x.shape[-1]
     if x.dim() > 2 or (k > 1 and x.stride(-1) != 1) or (x.shape[0] > 1 and x.stride(0) < k):
         x = x.contiguous()
-    rows = x.numel() // k
     kp = (k + 127) // 128 * 128
-    stride = k if x.dim() > 2 else _stride(x)
-    codes = torch.empty((*x.shape[:-1], kp // 2), dtype=torch.uint8, device=x.device)
-    scales = torch.empty((*x.shape[:-1], kp // 32), dtype=torch.uint8, device=x.device)
-    _call("gevo_mx4_quantize", x.device, DTYPES[x.dtype], rows, k, _ptr(x), stride, _ptr(codes), _ptr(scales))
-    return Mx4(codes, scales, k)
+    lead, dev = x.shape[:-1], x.device
+    q = Mx4.__new__(Mx4)
+    q.codes = torch.empty((*lead, kp // 2), dtype=torch.uint8, device=dev)
+    q.scales = torch.empty((*lead, kp // 32), dtype=torch.uint8, device=dev)
+    q.k = k
+    _call("gevo_mx4_quantize", dev, DTYPES[x.dtype], x.numel() // k, k, x.data_ptr(),
+          k if x.dim() > 2 else _stride(x), q.codes.data_ptr(), q.scales.data_ptr())
+    return q
 
 
 def mx4_matmul(a, b, *, bias=None, relu=False, plan=None, sorted_rows=False, out_dtype=torch.float32):
@@ -326,29 +375,36 @@ def mx4_matmul(a, b, *, bias=None, relu=False, plan=None, sorted_rows=False, out
     (gevo_mx4_matmul).  Without a plan [P][M][N], a being [M][K] for every p or
     [P][M][K]; with one the sorted rows [T k][N], a being [T][K] or, with
     sorted_rows, [T k][K]."""
-    _need(isinstance(a, Mx4) and isinstance(b, Mx4), "a, b: Mx4")
-    dev = a.codes.device
+    if not (isinstance(a, Mx4) and isinstance(b, Mx4)):
+        raise GevoError("a, b: Mx4")
+    ac, bc = a.codes, b.codes
+    dev = ac.device
     out_dtype = _out_dtype(out_dtype, torch.float32)
-    _need(len(b.shape) == 3 and b.codes.device == dev and a.k == b.k, f"b: [P][N][{a.k}] on {dev}, not {b.shape}")
-    P, N, K = b.shape
+    if bc.dim() != 3 or bc.device != dev or a.k != b.k:
+        raise GevoError(f"b: [P][N][{a.k}] on {dev}, not {b.shape}")
+    P, N, K = bc.shape[0], bc.shape[1], b.k
+    if P < 1 or N < 1:
+        raise GevoError(f"b: [P][N][K], not {b.shape}")
     if bias is not None:
         bias = _flat(bias, "bias", torch.float32, (P, N), dev)
-    k, order, offsets, each = 1, None, None, len(a.shape) == 3
+    k, order, offsets, each = 1, None, None, ac.dim() == 3
     if plan is None:
-        _need(len(a.shape) == 2 or a.shape[0] == P, f"a: [M][K] or [{P}][M][K], not {a.shape}")
-        _need(not sorted_rows, "sorted_rows: with a plan")
-        M = a.shape[-2]
+        if not (ac.dim() == 2 or (each and ac.shape[0] == P)):
+            raise GevoError(f"a: [M][K] or [{P}][M][K], not {a.shape}")
+        if sorted_rows:
+            raise GevoError("sorted_rows: with a plan")
+        M = ac.shape[-2]
         shape = (P, M, N)
     else:
-        _need(isinstance(plan, RoutePlan) and plan.pos.device == dev, f"plan: a RoutePlan on {dev}")
-        _need(plan.n_experts == P, f"b: {plan.n_experts} experts as the plan has, not {P}")
-        (M, k), order, offsets = plan.pos.shape, plan.order, plan.offsets
-        rows = M * k if sorted_rows else M
-        _need(tuple(a.shape) == (rows, K), f"a: shape {(rows, K)}, not {a.shape}")
+        _plan_of(plan, dev)
+        if plan.n_experts != P:
+            raise GevoError(f"b: {plan.n_experts} experts as the plan has, not {P}")
+        (M, k), order, offsets = plan.pos.shape, plan.order.data_ptr(), plan.offsets.data_ptr()
+        if a.shape != (M * k if sorted_rows else M, K):
+            raise GevoError(f"a: shape {(M * k if sorted_rows else M, K)}, not {a.shape}")
         shape = (M * k, N)
     out = torch.empty(shape, dtype=out_dtype, device=dev)
-    cfg = Mx4Config(GEVO_ABI_VERSION, DTYPES[out_dtype], P, N, K, M, 1 if each else 0, k, 1 if sorted_rows else 0,
-                    1 if relu else 0)
-    _call("gevo_mx4_matmul", dev, ctypes.byref(cfg), _ptr(a.codes), _ptr(a.scales), _ptr(b.codes), _ptr(b.scales),
-          _ptr(bias), _ptr(order), _ptr(offsets), _ptr(out))
+    cfg = _mx4_cfg(DTYPES[out_dtype], P, N, K, M, 1 if each else 0, k, 1 if sorted_rows else 0, 1 if relu else 0)
+    _call("gevo_mx4_matmul", dev, cfg, ac.data_ptr(), a.scales.data_ptr(), bc.data_ptr(), b.scales.data_ptr(),
+          _ptr(bias), order, offsets, out.data_ptr())
     return out
