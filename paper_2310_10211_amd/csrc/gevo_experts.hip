@@ -17,7 +17,6 @@
 #include "gevo_ops.h"
 
 #include <type_traits>
-#include <stdlib.h>  //TUNE
 
 namespace gevo {
 
@@ -851,12 +850,6 @@ hipError_t tile_shape(const ExpertArgs& a, hipStream_t s) {
   typedef typename Shapes<TY>::Wide Wide;
   typedef typename Shapes<TY>::Mid Mid;
   typedef typename Shapes<TY>::Small Small;
-  //TUNE
-  { const char* f = getenv("GEVO_SHAPE"); if (f && f[0]) {
-    if (f[0]=='0') return tile_go<Wide, TY, PASS, XL, WL, OUT16>(a, most_tiles<Wide>(a, PASS), s);
-    if (f[0]=='1') return tile_go<Mid, TY, PASS, XL, WL, OUT16>(a, most_tiles<Mid>(a, PASS), s);
-    return tile_go<Small, TY, PASS, XL, WL, OUT16>(a, most_tiles<Small>(a, PASS), s); } }
-  //TUNE
   const int64_t w = tile_time<Wide>(a, PASS, 10, 10), m = tile_time<Mid>(a, PASS, 13, 20),
                 n = tile_time<Small>(a, PASS, 20, 40);
   if (w <= m && w <= n) return tile_go<Wide, TY, PASS, XL, WL, OUT16>(a, most_tiles<Wide>(a, PASS), s);
