@@ -717,92 +717,113 @@ __global__ __launch_bounds__(SH::kThreads, SH::WGS* SH::kThreads / 256) void k_e
   }
 }
 
-// Few rows a segment: the weights' bytes are the time.  A workgroup takes 16
-// columns of one expert that has rows; its four waves split the contraction,
-// each reading its weights once, 16 x 64 bytes a load and eight loads ahead,
-// as one operand of a 16-row instruction whose other operand is up to 16 rows
-// of x.  The waves' sums are joined in LDS in the waves' order.
-template <ExpertType TY, bool VEC, bool OUT16>
-__global__ __launch_bounds__(256) void k_expert_few(ExpertArgs a) {
+// Few rows a segment: the weights' bytes are the time.  A wave takes 16 columns
+// of one expert that has rows and reads their weights once, 16 x 64 bytes a
+// load and eight loads ahead, as one operand of a 16-row instruction whose other
+// operand is up to 16 rows of x.  SPLIT: the four waves of a workgroup share 16
+// columns and split their contraction, and their sums are joined in LDS in the
+// waves' order.
+template <ExpertType TY, bool VEC, bool OUT16, bool SPLIT>
+__global__ __launch_bounds__(256, 4) void k_expert_few(ExpertArgs a) {
   typedef Mm<TY> M;
   typedef typename M::S S;
   constexpr bool mx = TY == kTypeMx4;
-  __shared__ f32x4_t part[4][64];
+  __shared__ f32x4_t part[SPLIT ? 4 : 1][64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l16 = lane & 15, lk = lane >> 4;
   int e = (int)blockIdx.y;
   if (a.offsets) {                                   // the blockIdx.y-th expert with rows
-  int left = (int)blockIdx.y, found = -1;
-  for (int b = 0; b < a.E && found < 0; b += 64) {
-    int64_t s0, cnt = 0;
-    if (b + lane < a.E) segment(a, b + lane, s0, cnt);
-    uint64_t in = __ballot(cnt > 0);
-    const int n = __popcll(in);
-    if (left < n) {
-      for (; left > 0; --left) in &= in - 1;
-      found = b + __ffsll((unsigned long long)in) - 1;
+    int left = (int)blockIdx.y, found = -1;
+    for (int b = 0; b < a.E && found < 0; b += 64) {
+      int64_t s0, cnt = 0;
+      if (b + lane < a.E) segment(a, b + lane, s0, cnt);
+      uint64_t in = __ballot(cnt > 0);
+      const int n = __popcll(in);
+      if (left < n) {
+        for (; left > 0; --left) in &= in - 1;
+        found = b + __ffsll((unsigned long long)in) - 1;
+      }
+      left -= n;
     }
-    left -= n;
-  }
-  if (found < 0) return;
-  e = __builtin_amdgcn_readfirstlane(found);
+    if (found < 0) return;
+    e = __builtin_amdgcn_readfirstlane(found);
   }
   int64_t s0, cnt;
   segment(a, e, s0, cnt);
-  const int n0 = blockIdx.x * 16, n = n0 + l16;
+  const int n0 = (SPLIT ? (int)blockIdx.x : (int)blockIdx.x * 4 + wave) * 16, n = n0 + l16;
+  if (!SPLIT && n0 >= a.N) return;
   const int bytes = mx ? (a.K + 127) / 128 * 64 : a.K * (int)sizeof(S);
-  const int nst = (bytes + 63) / 64, per = (nst + 3) / 4, st0 = wave * per, st1 = min(nst, st0 + per);
+  const int nst = (bytes + 63) / 64, per = SPLIT ? (nst + 3) / 4 : nst;
+  const int st0 = SPLIT ? wave * per : 0, st1 = min(nst, st0 + per);
   const char* wrow = (const char*)a.w + e * a.w_e + (n < a.N ? n : 0) * a.w_n + 16 * lk;
-  const char* wsrow = mx ? (const char*)a.ws + e * a.ws_e + (n < a.N ? n : 0) * a.ws_n + lk : nullptr;
+  const char* wsrow = mx ? (const char*)a.ws + e * a.ws_e + (n < a.N ? n : 0) * a.ws_n : nullptr;
   for (int64_t m0 = 0; m0 < cnt; m0 += 16) {
-  const int64_t i = m0 + l16;
-  const int64_t r = i < cnt ? source_row(a, s0, i) : -1;
-  const int64_t xe = a.offsets ? 0 : (int64_t)e;
-  const char* xrow = (const char*)a.x + xe * a.x_e + (r < 0 ? 0 : r) * a.x_stride + 16 * lk;
-  const char* xsrow = mx ? (const char*)a.xs + xe * a.xs_e + (r < 0 ? 0 : r) * a.xs_stride + lk : nullptr;
-  f32x4_t acc = {0.0f, 0.0f, 0.0f, 0.0f};
-  auto load = [&](const char* p, bool have, int st) -> uint4 {
-    const int left = bytes - st * 64 - 16 * lk;
-    if constexpr (VEC || mx) {
-      return have && left > 0 ? *reinterpret_cast<const uint4*>(p + st * 64) : make_uint4(0, 0, 0, 0);
-    } else {
-      return load_chunk<S>(p + st * 64, have ? left / (int)sizeof(S) : 0);
-    }
-  };
-  constexpr int U = 8;
-  for (int b = st0; b < st1; b += U) {
-    uint4 fw[U], fx[U];
-    uint32_t sw[U], sx[U];
+    const int64_t i = m0 + l16;
+    const int64_t r = i < cnt ? source_row(a, s0, i) : -1;
+    const int64_t xe = a.offsets ? 0 : (int64_t)e;
+    const char* xrow = (const char*)a.x + xe * a.x_e + (r < 0 ? 0 : r) * a.x_stride + 16 * lk;
+    const char* xsrow = mx ? (const char*)a.xs + xe * a.xs_e + (r < 0 ? 0 : r) * a.xs_stride : nullptr;
+    f32x4_t acc = {0.0f, 0.0f, 0.0f, 0.0f};
+    auto load = [&](const char* p, bool have, int st) -> uint4 {
+      const int left = bytes - st * 64 - 16 * lk;
+      if constexpr (VEC || mx) {
+        return have && left > 0 ? *reinterpret_cast<const uint4*>(p + st * 64) : make_uint4(0, 0, 0, 0);
+      } else {
+        return load_chunk<S>(p + st * 64, have ? left / (int)sizeof(S) : 0);
+      }
+    };
+    constexpr int U = 8;
+    // the scales of U steps, 4 bytes (one a chunk lane) each, the lane's first
+    auto scales = [&](const char* p, bool have, int b, uint32_t (&v)[U]) {
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const bool in = b + u < st1;
-      fw[u] = load(wrow, in && n < a.N, b + u);
-      fx[u] = load(xrow, in && r >= 0, b + u);
-      sw[u] = sx[u] = 0;
+      for (int u = 0; u < U; u += 4) {
+        uint32_t q[4] = {0, 0, 0, 0};
+        if (have && b + u + 4 <= st1) {
+          __builtin_memcpy(q, __builtin_assume_aligned(p + (b + u) * 4, 4), 16);
+        } else if (have) {
+#pragma unroll
+          for (int d = 0; d < 4; ++d)
+            if (b + u + d < st1) q[d] = *reinterpret_cast<const uint32_t*>(p + (b + u + d) * 4);
+        }
+#pragma unroll
+        for (int d = 0; d < 4; ++d) v[u + d] = q[d] >> (8 * lk);
+      }
+    };
+    for (int b = st0; b < st1; b += U) {
+      uint4 fw[U], fx[U];
+      uint32_t sw[U], sx[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const bool in = b + u < st1;
+        fw[u] = load(wrow, in && n < a.N, b + u);
+        fx[u] = load(xrow, in && r >= 0, b + u);
+        sw[u] = sx[u] = 0;
+      }
       if constexpr (mx) {
-        if (in && n < a.N) sw[u] = (uint8_t)wsrow[(b + u) * 4];
-        if (in && r >= 0) sx[u] = (uint8_t)xsrow[(b + u) * 4];
+        scales(wsrow, n < a.N, b, sw);
+        scales(xsrow, r >= 0, b, sx);
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) acc = M::mma16(fw[u], fx[u], acc, sw[u], sx[u]);
+    }
+    if constexpr (SPLIT) {
+      __syncthreads();                               // the last tile's sums have been read
+      part[wave][lane] = acc;
+      __syncthreads();
+      acc = part[0][lane] + part[1][lane] + part[2][lane] + part[3][lane];
+    }
+    if ((!SPLIT || wave == 0) && r >= 0) {           // lane: row l16, columns n0 + 4 lk + 0 .. 3
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int c = n0 + 4 * lk + u;
+        if (c >= a.N) continue;
+        float f = acc[u];
+        if (a.bias) f += a.bias[(int64_t)e * a.N + c];
+        if (a.relu) f = f < 0.0f ? 0.0f : f;         // (NaN stays)
+        const int64_t at = (s0 + i) * a.out_stride + c;
+        if constexpr (OUT16) ((uint16_t*)a.out)[at] = f32_to_bf16_bits(f);
+        else ((float*)a.out)[at] = f;
       }
     }
-#pragma unroll
-    for (int u = 0; u < U; ++u) acc = M::mma16(fw[u], fx[u], acc, sw[u], sx[u]);
-  }
-  __syncthreads();                                 // the last tile's sums have been read
-  part[wave][lane] = acc;
-  __syncthreads();
-  if (wave == 0 && r >= 0) {                       // lane: row l16, columns n0 + 4 lk + 0 .. 3
-    const f32x4_t sum = part[0][lane] + part[1][lane] + part[2][lane] + part[3][lane];
-#pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      const int c = n0 + 4 * lk + u;
-      if (c >= a.N) continue;
-      float f = sum[u];
-      if (a.bias) f += a.bias[(int64_t)e * a.N + c];
-      if (a.relu) f = f > 0.0f || f != f ? f : 0.0f;
-      const int64_t at = (s0 + i) * a.out_stride + c;
-      if constexpr (OUT16) ((uint16_t*)a.out)[at] = f32_to_bf16_bits(f);
-      else ((float*)a.out)[at] = f;
-    }
-  }
   }
 }
 
@@ -861,6 +882,19 @@ bool aligned16(const void* p, int64_t a, int64_t b, int64_t c) {
   return ((uintptr_t)p | (uintptr_t)a | (uintptr_t)b | (uintptr_t)c) % 16 == 0;
 }
 
+// The contraction is split where 16 columns a wave would leave the chip less
+// than eight waves a CU, if each of its parts is a few loads long.
+template <ExpertType TY, bool VEC, bool OUT16>
+hipError_t few_go(const ExpertArgs& a, int64_t segs, hipStream_t s) {
+  const int64_t bands = (a.N + 15) / 16;
+  const int64_t bytes = TY == kTypeMx4 ? (a.K + 127) / 128 * 64 : a.K * (int64_t)sizeof(typename Mm<TY>::S);
+  if (bands * segs < 2048 && bytes >= 1024)
+    k_expert_few<TY, VEC, OUT16, true><<<dim3((unsigned)bands, (unsigned)segs), 256, 0, s>>>(a);
+  else
+    k_expert_few<TY, VEC, OUT16, false><<<dim3((unsigned)((bands + 3) / 4), (unsigned)segs), 256, 0, s>>>(a);
+  return hipGetLastError();
+}
+
 template <ExpertType TY, bool OUT16>
 hipError_t forward_out(const ExpertArgs& a, hipStream_t s) {
   const bool vec = TY == kTypeMx4 || (aligned16(a.x, a.x_stride, a.x_e, a.K * (int64_t)sizeof(typename Mm<TY>::S)) &&
@@ -868,10 +902,7 @@ hipError_t forward_out(const ExpertArgs& a, hipStream_t s) {
   // Up to 16 rows a segment on average the weights' bytes bound the product
   const int64_t segs = a.offsets ? (a.S < a.E ? a.S : a.E) : a.E;
   if (a.S <= segs * 16 && segs <= 65535) {
-    const dim3 grid((unsigned)((a.N + 15) / 16), (unsigned)segs);
-    if (vec) k_expert_few<TY, true, OUT16><<<grid, 256, 0, s>>>(a);
-    else k_expert_few<TY, false, OUT16><<<grid, 256, 0, s>>>(a);
-    return hipGetLastError();
+    return vec ? few_go<TY, true, OUT16>(a, segs, s) : few_go<TY, false, OUT16>(a, segs, s);
   }
   if constexpr (TY == kTypeMx4) return tile_shape<TY, kForward, kDma, kDma, OUT16>(a, s);
   else if (vec) return tile_shape<TY, kForward, kDma, kDma, OUT16>(a, s);

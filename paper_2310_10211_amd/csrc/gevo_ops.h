@@ -18,6 +18,7 @@ struct RouteArgs {
   int64_t T;
   int E, k, groups, top_groups, group_top;
   int sigmoid, renorm, by_logit;       // by_logit: the logits themselves are the keys
+  int vec;                             // set by the launcher: rows are aligned and fill the lanes
   float scale;
   float* weights; int32_t* ids;        // [T][k]
   const float* dweights;               // backward: [T][k]

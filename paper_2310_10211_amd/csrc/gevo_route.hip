@@ -29,11 +29,33 @@ __device__ __forceinline__ float exp_split(float x) {
   return fmaf(e, r * 0.693147182f, e);
 }
 
-// Reductions over the L lanes (16 or 64, aligned) that share a row.
+// A value rotated by N lanes within each 16.
+template <int N>
+__device__ __forceinline__ int rotated(int v) {
+  return __builtin_amdgcn_update_dpp(v, v, 0x120 + N, 0xf, 0xf, false);
+}
+
+// Reductions over the L lanes (16 or 64, aligned) that share a row; f is
+// commutative.  32-bit values: rotations within 16 lanes, which cost an
+// instruction each, then the four sixteens' values from scalar registers.
 template <int L, typename T, typename F>
 __device__ __forceinline__ T row_reduce(T v, F f) {
+  if constexpr (sizeof(T) == 4) {
+    v = f(v, __builtin_bit_cast(T, rotated<8>(__builtin_bit_cast(int, v))));
+    v = f(v, __builtin_bit_cast(T, rotated<4>(__builtin_bit_cast(int, v))));
+    v = f(v, __builtin_bit_cast(T, rotated<2>(__builtin_bit_cast(int, v))));
+    v = f(v, __builtin_bit_cast(T, rotated<1>(__builtin_bit_cast(int, v))));
+    if constexpr (L == 64) {
+      T q[4];
 #pragma unroll
-  for (int m = L / 2; m >= 1; m >>= 1) v = f(v, __shfl_xor(v, m, L));
+      for (int i = 0; i < 4; ++i)
+        q[i] = __builtin_bit_cast(T, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), 16 * i));
+      v = f(f(q[0], q[1]), f(q[2], q[3]));
+    }
+  } else {
+#pragma unroll
+    for (int m = L / 2; m >= 1; m >>= 1) v = f(v, __shfl_xor(v, m, L));
+  }
   return v;
 }
 template <int L>
@@ -49,9 +71,10 @@ __device__ __forceinline__ uint64_t row_ballot(bool p) {
 // groups of keys, then the k largest keys among them (descending, ties to the
 // lowest index), weights scale s (renormalised over the choice).
 //
-// L lanes share a row, each holding NE consecutive logits, so a tie's lowest
-// index is the lowest lane's first.  A maximum over the row is a local one and
-// log2 L shuffles; taking an element out redoes its lane's local maximum.
+// L lanes share a row, each holding NE consecutive logits.  A choice is the
+// row's largest local maximum and the lowest index that holds it; taking it out
+// redoes its lane's local maximum.  Bound by these instructions: a row of 256
+// logits needs about 90 for each choice of four rows.
 //
 // Two keys nearer than the rounding of 32-bit scores would be ordered by that
 // rounding: a row with such a pair among the keys (or groups) that decide its
@@ -69,8 +92,19 @@ __global__ __launch_bounds__(256) void k_route(RouteArgs a) {
   const float ninf = -INFINITY;
 
   float l[NE];
+  if (a.vec) {                                       // whole rows of aligned chunks
+    constexpr int V = 16 / sizeof(S) < NE ? 16 / sizeof(S) : NE;
 #pragma unroll
-  for (int j = 0; j < NE; ++j) l[j] = live && e0 + j < a.E ? to_f<S>(lrow[e0 + j]) : ninf;
+    for (int j = 0; j < NE; j += V) {
+      S e[V];
+      __builtin_memcpy(e, __builtin_assume_aligned(lrow + e0 + j, V * sizeof(S)), sizeof(e));
+#pragma unroll
+      for (int v = 0; v < V; ++v) l[j + v] = live ? to_f<S>(e[v]) : ninf;
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < NE; ++j) l[j] = live && e0 + j < a.E ? to_f<S>(lrow[e0 + j]) : ninf;
+  }
 
   bool bad = false;                                  // NaN, or +inf under softmax: no scores
   float m = ninf;
@@ -106,24 +140,31 @@ __global__ __launch_bounds__(256) void k_route(RouteArgs a) {
 #pragma unroll
       for (int j = 0; j < NE; ++j) key[j] = (F)l[j];
     } else {
-#pragma unroll
-      for (int j = 0; j < NE; ++j) {
-        if constexpr (wide) key[j] = a.sigmoid ? 1.0 / (1.0 + exp(-(double)l[j])) : exp((double)l[j] - (double)m);
-        else key[j] = a.sigmoid ? 1.0f / (1.0f + exp_split(fminf(-l[j], 88.0f))) : exp_split(l[j] - m);
-        if (l[j] == ninf) key[j] = 0;
-        sum += key[j];
-      }
       F top = 1;
-      if (!a.sigmoid) {
+      if (a.sigmoid) {
+#pragma unroll
+        for (int j = 0; j < NE; ++j) {
+          if constexpr (wide) key[j] = 1.0 / (1.0 + exp(-(double)l[j]));
+          else key[j] = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(l[j] * -1.44269504f));
+        }
+      } else {
+#pragma unroll
+        for (int j = 0; j < NE; ++j) {
+          if constexpr (wide) key[j] = l[j] == ninf ? 0.0 : exp((double)l[j] - (double)m);
+          else key[j] = l[j] == ninf ? 0.0f : __builtin_amdgcn_exp2f((l[j] - m) * 1.44269504f);
+          sum += key[j];
+        }
         sum = row_reduce<L>(sum, [](F x, F y) { return x + y; });
         top = (F)1 / sum;                            // the row's largest score
 #pragma unroll
         for (int j = 0; j < NE; ++j) key[j] *= top;
       }
-      // twice what two 32-bit keys can be off by: 2e-7 of a sigmoid, 4e-6 of a
-      // softmax (its logit differences, to 40 below the largest, and sum), half a
-      // step of the sum with the bias; a group adds two keys
-      if (!wide) tol = 4 * ((a.sigmoid ? 2e-7f : 4e-6f) * top + 6e-8f * (top + (F)bmax)) * a.group_top;
+      // What two keys in 32 bits can be off by together.  exp2's argument is
+      // rounded to |x| 2^-24 log2 e, which x s (1 - s) <= 0.23 and d e^-d <= 0.37
+      // keep below 4e-8 of a score; its result, the sum with 1 and the reciprocal
+      // add a step (1.2e-7) each at most, the sum over a row 4e-7, the sum with
+      // the bias half a step of itself; a group adds two keys.
+      if (!wide) tol = 2 * ((a.sigmoid ? 5e-7f : 1e-6f) * top + 6e-8f * (top + (F)bmax)) * a.group_top;
 #pragma unroll
       for (int j = 0; j < NE; ++j) {
         if (a.bias && e0 + j < a.E) key[j] += (F)a.bias[e0 + j];
@@ -132,19 +173,36 @@ __global__ __launch_bounds__(256) void k_route(RouteArgs a) {
     }
     bool sure = true;
     if (a.groups > 1) {
-      F* ks = reinterpret_cast<F*>(smem) + (size_t)rw * (L * NE);
+      // a group's value, in every lane that holds part of it: from registers where
+      // 1, 2, 4 .. whole lanes hold a group, else through LDS (lane g: group g)
+      const int per = gs / NE;                       // lanes of a group
+      const bool inreg = gs % NE == 0 && (per & (per - 1)) == 0;
+      F v1 = lowest, v2 = lowest;                    // its largest keys
+      auto take = [&](F x) {
+        v2 = x > v1 ? v1 : (x > v2 ? x : v2);
+        v1 = x > v1 ? x : v1;
+      };
+      int mine = lane;                               // the group whose value the lane holds
+      if (inreg) {
 #pragma unroll
-      for (int j = 0; j < NE; ++j) ks[e0 + j] = key[j];
-      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-      F v1 = lowest, v2 = lowest;                    // lane g: the largest keys of group g
-      if (lane < a.groups)
-        for (int i = 0; i < gs; ++i) {
-          const F x = ks[lane * gs + i];
-          v2 = x > v1 ? v1 : (x > v2 ? x : v2);
-          v1 = x > v1 ? x : v1;
+        for (int j = 0; j < NE; ++j) take(key[j]);
+        for (int d = 1; d < per; d <<= 1) {
+          const F o1 = __shfl_xor(v1, d, L), o2 = __shfl_xor(v2, d, L);
+          take(o1);
+          take(o2);
         }
+        mine = lane / per;
+      } else {
+        F* ks = reinterpret_cast<F*>(smem) + (size_t)rw * (L * NE);
+#pragma unroll
+        for (int j = 0; j < NE; ++j) ks[e0 + j] = key[j];
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        if (lane < a.groups)
+          for (int i = 0; i < gs; ++i) take(ks[lane * gs + i]);
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      }
       F v = a.group_top == 2 && v2 > lowest ? v1 + v2 : v1;
-      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      if (mine >= a.groups) v = lowest;
       uint64_t stay = 0;
       F last = lowest;
       for (int i = 0; i <= a.top_groups && i < a.groups; ++i) {
@@ -153,17 +211,22 @@ __global__ __launch_bounds__(256) void k_route(RouteArgs a) {
           if (!(last - mx > tol) && last > lowest) sure = false;
           break;
         }
-        const uint64_t at = row_ballot<L>(v == mx && lane < a.groups);
-        const int g = __ffsll((unsigned long long)at) - 1;
-        if (g >= 0) stay |= 1ull << g;
+        const int g = row_reduce<L>(v == mx && mine < a.groups ? mine : 64, [](int x, int y) { return x < y ? x : y; });
+        if (g < 64) stay |= 1ull << g;
         last = mx;
-        if (lane == g) v = lowest;
+        if (mine == g) v = lowest;
       }
-      int g = e0 / gs, left = (g + 1) * gs - e0;
+      if (inreg) {
+        const bool in = (stay >> (mine & 63)) & 1;
 #pragma unroll
-      for (int j = 0; j < NE; ++j) {
-        if (!((stay >> (g & 63)) & 1)) key[j] = lowest;
-        if (--left == 0) { ++g; left = gs; }
+        for (int j = 0; j < NE; ++j) key[j] = in ? key[j] : lowest;
+      } else {
+        int g = e0 / gs, left = (g + 1) * gs - e0;
+#pragma unroll
+        for (int j = 0; j < NE; ++j) {
+          if (!((stay >> (g & 63)) & 1)) key[j] = lowest;
+          if (--left == 0) { ++g; left = gs; }
+        }
       }
     }
     F lm = lowest;
@@ -171,26 +234,24 @@ __global__ __launch_bounds__(256) void k_route(RouteArgs a) {
     for (int j = 0; j < NE; ++j) lm = key[j] > lm ? key[j] : lm;
     chosen = -1;
     F last = lowest;
-    for (int i = 0; i <= a.k; ++i) {
+    const int tries = wide || a.by_logit ? a.k : a.k + 1;   // the first key left out is looked at, too
+    for (int i = 0; i < tries; ++i) {
       const F mx = row_reduce<L>(lm, [](F x, F y) { return x > y ? x : y; });
       if (i > 0 && !wide && !a.by_logit && last > lowest && !(last - mx > tol)) sure = false;
       if (i == a.k) break;
       last = mx;
-      const int win = __ffsll((unsigned long long)row_ballot<L>(lm == mx && mx > lowest)) - 1;
-      int at = -1;
-      if (lane == win) {
+      int at = NE;                                   // the first of the lane's that is as large
 #pragma unroll
-        for (int j = NE - 1; j >= 0; --j)
-          if (key[j] == mx) at = j;
-        lm = lowest;
+      for (int j = NE - 1; j >= 0; --j) at = key[j] == mx ? j : at;
+      const int none = 1 << 30;
+      const int e = row_reduce<L>(at < NE && mx > lowest ? e0 + at : none, [](int x, int y) { return x < y ? x : y; });
+      if (lane == i) chosen = e < none ? e : -1;
+      lm = lowest;
 #pragma unroll
-        for (int j = 0; j < NE; ++j) {
-          if (j == at) key[j] = lowest;
-          lm = key[j] > lm ? key[j] : lm;
-        }
+      for (int j = 0; j < NE; ++j) {
+        key[j] = e0 + j == e ? lowest : key[j];
+        lm = key[j] > lm ? key[j] : lm;
       }
-      const int e = win < 0 ? -1 : __shfl(e0 + at, win & (L - 1), L);
-      if (lane == i) chosen = e;
     }
     return sure;
   };
@@ -321,12 +382,18 @@ namespace {
 
 // Lanes and logits a lane: 16 lanes where the row and the choice fit them.  Four
 // rows to a wave make a maximum over the row four shuffles for the four.
+size_t route_lds(const RouteArgs& a, int rows, int L, int NE) {
+  const int gs = a.E / a.groups, per = gs / NE;
+  return a.groups == 1 || (gs % NE == 0 && (per & (per - 1)) == 0) ? 0 : (size_t)rows * L * NE * 8;
+}
 template <typename S, bool BWD, int L, int NE>
-hipError_t route_go(const RouteArgs& a, hipStream_t s) {
-  constexpr int rows = 256 / L;
+hipError_t route_go(const RouteArgs& args, hipStream_t s) {
+  constexpr int rows = 256 / L, align = NE * sizeof(S) < 16 ? NE * sizeof(S) : 16;
+  RouteArgs a = args;
+  a.vec = a.E == L * NE && (uintptr_t)a.logits % align == 0 && a.stride * (int64_t)sizeof(S) % align == 0;
   const unsigned grid = (unsigned)((a.T + rows - 1) / rows);
   if (BWD) k_route_bwd<S, L, NE><<<grid, 256, (size_t)rows * L * NE * 4, s>>>(a);
-  else k_route<S, L, NE><<<grid, 256, a.groups > 1 ? (size_t)rows * L * NE * 8 : 0, s>>>(a);
+  else k_route<S, L, NE><<<grid, 256, route_lds(a, rows, L, NE), s>>>(a);
   return hipGetLastError();
 }
 
