@@ -439,6 +439,24 @@ class Population:
                                             b.data_ptr()), "gevo_pop_layer_weights")
         return w, b
 
+    def predict_mx4(self) -> dict:
+        """The prediction workload with every layer's weights and inputs in
+        microscaled 4 bits: test_loss and test_acc [P] of the test split.  Chunks
+        of rows bound the memory of the hidden activations."""
+        torch = self.torch
+        from .mixture import Mixture, scores
+        with torch.cuda.stream(self.stream):
+            m = Mixture(self, numerics="mx4")
+            loss = torch.zeros(self.P, dtype=torch.float64, device=self.workspace.device)
+            acc = torch.zeros_like(loss)
+            chunk = max(64, (1 << 29) // (self.P * max(self.dims[1:])))
+            for r in range(0, self.n_test, chunk):
+                x, y = self.x_test[r:r + chunk], self.y_test[r:r + chunk]
+                mean, right = scores(m.predict_all(x), y)
+                loss += mean.double() * (len(x) / self.n_test)
+                acc += right.double() * (len(x) / self.n_test)
+            return {"test_loss": loss.float().cpu().numpy(), "test_acc": acc.float().cpu().numpy()}
+
     def epoch_labels(self) -> np.ndarray:
         out = np.zeros(self.n_train, np.int32)
         _check(lib().gevo_pop_epoch_labels(self._h, out.ctypes.data_as(ctypes.POINTER(ctypes.c_int32)),

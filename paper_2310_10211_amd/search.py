@@ -24,7 +24,9 @@ Each generation keeps the n_elite best unchanged and fills the rest with the
 children of tournament winners (section 4.4).  The elites keep the fitness
 they were selected with: the whole generation is retrained as one population,
 but an unchanged individual is not scored again (a variant's rounding can
-depend on its slot in the population).  All computation happens in
+depend on its slot in the population).  The test split's error, which checks
+the front afterwards, is of the population's own prediction or, with
+test_numerics "mx4", of its prediction in microscaled 4 bits.  All computation happens in
 libgevo; this module only marshals arguments and keeps the history.
 """
 from __future__ import annotations
@@ -49,12 +51,14 @@ class Generation:
 class Search:
     def __init__(self, pop: Population, lr_base: float, seed: int, epochs: int = 1, rho_lo: float = 0.3,
                  n_elite: int = 16, cxpb: float = 0.8, mutpb: float = 0.5, max_edits: int = 16, n_mut: int = 3,
-                 struct_p: float = 0.0, time_objective: str = "kept"):
+                 struct_p: float = 0.0, time_objective: str = "kept", test_numerics: str = "population"):
         if not 0 <= n_elite <= pop.P:
             raise ValueError("n_elite must be in [0, P]")
         if time_objective not in ("kept", "measured"):
             raise ValueError("time_objective must be 'kept' or 'measured'")
-        self.time_objective = time_objective
+        if test_numerics not in ("population", "mx4"):
+            raise ValueError("test_numerics must be 'population' or 'mx4'")
+        self.time_objective, self.test_numerics = time_objective, test_numerics
         self.pop, self.lr_base, self.seed, self.epochs = pop, float(lr_base), int(seed), int(epochs)
         self.rho_lo, self.n_elite, self.cxpb, self.mutpb = float(rho_lo), int(n_elite), float(cxpb), float(mutpb)
         self.max_edits, self.n_mut, self.struct_p = int(max_edits), int(n_mut), float(struct_p)
@@ -75,7 +79,8 @@ class Search:
         train_err = 1.0 - np.asarray(s["train_acc"], np.float64)
         cost = dens if self.time_objective == "kept" else t + np.asarray(s["time_s"], np.float64)
         objs = np.stack([train_err, cost], axis=1)
-        test_err = 1.0 - np.asarray(s["test_acc"], np.float64)
+        test_acc = pop.predict_mx4()["test_acc"] if self.test_numerics == "mx4" else s["test_acc"]
+        test_err = 1.0 - np.asarray(test_acc, np.float64)
         if carried is not None:
             k = len(carried[0])
             objs[:k] = carried[0]
