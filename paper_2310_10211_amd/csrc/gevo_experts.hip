@@ -228,25 +228,42 @@ __device__ __forceinline__ bool find_tile(const ExpertArgs& a, int ntiles, Tile&
   return true;
 }
 
-// 16 bytes at p, which has its element's alignment, of which the first `valid`
-// elements exist
+// The elements of a row's last 16 bytes u from the drop-th on, then zeros.
 template <typename S>
-__device__ __forceinline__ uint4 load_chunk(const char* p, int valid) {
-  constexpr int V = 16 / sizeof(S);
-  if (valid <= 0) return make_uint4(0, 0, 0, 0);
-  uint4 u;
-  if (valid >= V) {
-    __builtin_memcpy(&u, p, 16);                     // one load, at any address
-    return u;
-  }
-  S e[V];
-#pragma unroll
-  for (int i = 0; i < V; ++i) e[i] = i < valid ? reinterpret_cast<const S*>(p)[i] : (S)0;
-  __builtin_memcpy(&u, e, 16);
+__device__ __forceinline__ uint4 without_first(uint4 u, int drop) {
+  if (sizeof(S) == 2 && (drop & 1))
+    u = make_uint4(__builtin_amdgcn_alignbit(u.y, u.x, 16), __builtin_amdgcn_alignbit(u.z, u.y, 16),
+                   __builtin_amdgcn_alignbit(u.w, u.z, 16), u.w >> 16);
+  const int d = sizeof(S) == 2 ? drop >> 1 : drop;
+  if (d & 1) u = make_uint4(u.y, u.z, u.w, 0);
+  if (d & 2) u = make_uint4(u.z, u.w, 0, 0);
   return u;
 }
 
-enum Load { kDma, kGuarded, kTransposed };
+// 16 bytes at p, which has its element's alignment, of which the first `valid`
+// elements exist (at most 0: none, and zeros).  edge: some lane's chunk may be
+// the last, partly filled one of its row; it is then read as the row's last 16
+// bytes, less the elements before it.  Rows of less than 16 bytes (not wide) are
+// read element by element.  Loads of absent chunks go to `safe`, so that no
+// lane branches and all of a wave's loads are under way together.
+template <typename S>
+__device__ __forceinline__ uint4 load_chunk(const char* p, int valid, bool edge, bool wide, const char* safe) {
+  constexpr int V = 16 / sizeof(S);
+  uint4 u;
+  if (!wide) {
+    S e[V];
+#pragma unroll
+    for (int i = 0; i < V; ++i) e[i] = i < valid ? reinterpret_cast<const S*>(p)[i] : (S)0;
+    __builtin_memcpy(&u, e, 16);
+    return u;
+  }
+  const int drop = edge && valid < V ? V - valid : 0;
+  __builtin_memcpy(&u, valid > 0 ? p - drop * (int)sizeof(S) : safe, 16);   // one load, at any address
+  if (edge) u = without_first<S>(u, drop);
+  return valid > 0 ? u : make_uint4(0, 0, 0, 0);
+}
+
+enum Load { kDma, kGuarded, kTransposed, kNatural };
 enum Pass { kForward, kDx, kDw };
 
 }  // namespace
@@ -255,8 +272,12 @@ enum Pass { kForward, kDx, kDw };
 //   kDma         16-byte chunks straight to LDS, a step ahead
 //   kGuarded     through registers, at any address, where rows are not aligned
 //                or the contraction ends inside a chunk
-//   kTransposed  the contraction is the operand's outer index: a lane loads a
-//                square of 8 x 8 (fp32: 4 x 4) values and turns it in registers
+//   kNatural     the contraction is the operand's outer index: rows of one
+//                contraction index each, straight to LDS; bf16 operands are read
+//                with gfx950's transposing LDS read (each 16 lanes a 4 x 16 block
+//                by columns), fp32 ones value by value
+//   kTransposed  the same at any address or width: a lane loads a square of
+//                8 x 8 (fp32: 4 x 4) values and turns it in registers
 template <typename SH, ExpertType TY, Pass PASS, Load XL, Load WL, bool OUT16>
 __global__ __launch_bounds__(SH::kThreads, SH::WGS* SH::kThreads / 256) void k_expert_tile(ExpertArgs a) {
   typedef Mm<TY> M;
@@ -268,8 +289,9 @@ __global__ __launch_bounds__(SH::kThreads, SH::WGS* SH::kThreads / 256) void k_e
   constexpr int kStep = SH::kStep, kC = kStep / 16, kQ = kStep / 32;   // chunks, parts of a step
   constexpr bool mx = TY == kTypeMx4;
   constexpr int kBuf = kXBytes + kWBytes + (mx ? SH::kScaleBytes : 0);
-  constexpr bool kAllDma = XL == kDma && WL == kDma;
-  constexpr int kIssued = (XL == kDma ? NXL : 0) + (WL == kDma ? NWL : 0) + (mx ? kC / 4 : 0);   // a step and wave
+  constexpr bool kAllDma = (XL == kDma || XL == kNatural) && (WL == kDma || WL == kNatural);
+  constexpr int kXi = XL == kDma || XL == kNatural ? NXL : 0, kWi = WL == kDma || WL == kNatural ? NWL : 0;
+  constexpr int kIssued = kXi + kWi + (mx ? kC / 4 : 0);   // loads straight to LDS a step and wave
   extern __shared__ __align__(16) char smem[];
 
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l32 = lane & 31, lh = lane >> 5;
@@ -328,6 +350,9 @@ __global__ __launch_bounds__(SH::kThreads, SH::WGS* SH::kThreads / 256) void k_e
   const char* sq_p = nullptr;                        // contraction row 0, the square's first column
   int64_t sq_stride = 0;
   int sq_valid = 0;                                  // columns that exist
+  // the tiles' columns: all there; rows of at least 16 bytes
+  const bool sq_edge = n0 + kWR > cols || (PASS == kDw && tl.m0 + kXR > a.N);
+  const bool sq_wide = cols >= V && (PASS != kDw || a.N >= V);
   int32_t sq_row[kTr ? V : 1];                       // rows of the step to fetch next
   float dbs[V];
 
@@ -381,22 +406,83 @@ __global__ __launch_bounds__(SH::kThreads, SH::WGS* SH::kThreads / 256) void k_e
     }
   }
 
+  // ---- natural order: a load's 1,024 bytes are 1,024 / kRowBytes rows of one
+  // contraction index each.  So that the reads below cover the banks, 64-byte
+  // blocks of bf16 rows change places with the index mod 4 (rows of 128 bytes:
+  // with its second bit), 128-byte blocks of fp32 rows with its third bit.
+  struct Natural {                                   // of one operand
+    const char* base;                                // contraction row 0
+    int64_t stride;
+    int row0, per;                                   // the lane's row in the wave's first load; rows a load
+    int cb[2];                                       // its column's byte in even and odd loads, -1: none
+    int drop[2];                                     // elements of the chunk before that column
+  } nx{}, nw{};
+  auto natural_block = [](int tile_bytes, int row) {  // what the row's 16-byte chunks are xored with
+    if (sizeof(S) == 4) return ((row >> 2) & 1) << 3;
+    return (tile_bytes == 128 ? (row >> 1) & 1 : row & 3) << 2;
+  };
+  auto natural_setup = [&](Natural& d, const char* base, int64_t stride, int tile_rows, int loads, int col0, int width) {
+    const int tb = tile_rows * (int)sizeof(S);       // bytes of a tile's row
+    d.base = base;
+    d.stride = stride;
+    d.per = 1024 / tb;
+    d.row0 = loads * wave * d.per + lane / (tb / 16);
+#pragma unroll
+    for (int v = 0; v < 2; ++v) {
+      const int ch = lane % (tb / 16) ^ natural_block(tb, d.row0 + v * d.per);
+      const int c = col0 * (int)sizeof(S) + 16 * ch;
+      const int over = c + 16 - width * (int)sizeof(S);   // as below
+      d.drop[v] = over > 0 && over < 16 ? over / (int)sizeof(S) : 0;
+      d.cb[v] = over < 16 ? c - (over > 0 ? over : 0) : -1;
+    }
+  };
+  if constexpr (XL == kNatural)                      // dw: columns of dy
+    natural_setup(nx, (const char*)a.w + tl.s0 * a.w_n, a.w_n, kXR, NXL, (int)tl.m0, a.N);
+  if constexpr (WL == kNatural) {
+    if constexpr (PASS == kDw) natural_setup(nw, (const char*)a.x, a.x_stride, kWR, NWL, n0, a.K);
+    else natural_setup(nw, (const char*)a.w + tl.e * a.w_e, a.w_n, kWR, NWL, n0, a.N);
+  }
+  int32_t gathered[PASS == kDw && WL == kNatural ? NWL : 1];   // rows of x that the next step's loads read
+  auto gather = [&](int st) {
+    if constexpr (PASS == kDw && WL == kNatural) {
+#pragma unroll
+      for (int n = 0; n < NWL; ++n) {
+        const int64_t k = (int64_t)st * kPer + nw.row0 + n * nw.per;
+        gathered[n] = k < clen ? (int32_t)source_row(a, tl.s0, k) : -1;
+      }
+    }
+  };
+
   // load n of the wave's kIssued loads of step st, to buffer b
   auto issue_one = [&](int st, int b, int n) {
     const uint32_t buf = scalar(lds0 + (uint32_t)b * kBuf);
     const int at = st * kStep;
-    if (XL == kDma && n < NXL) {
-      const bool in = (have >> n & 1) && at + cb[n & 1] < bytes;
-      dma16_at(in ? xp[n] + at : zero, buf + (uint32_t)(NXL * wu + n) * 1024u);
+    if (n < kXi) {
+      const uint32_t to = buf + (uint32_t)(NXL * wu + n) * 1024u;
+      if constexpr (XL == kDma) {
+        const int over = at + cb[n & 1] + 16 - bytes;  // bytes of the chunk past the row
+        dma16_at((have >> n & 1) && over < 16 ? xp[n] + at - (over > 0 ? over : 0) : zero, to);
+      } else {
+        const int64_t k = (int64_t)st * kPer + nx.row0 + n * nx.per;
+        dma16_at(k < clen && nx.cb[n & 1] >= 0 ? nx.base + k * nx.stride + nx.cb[n & 1] : zero, to);
+      }
       return;
     }
-    if (XL == kDma) n -= NXL;
-    if (WL == kDma && n < NWL) {
-      const bool in = (have >> (16 + n) & 1) && at + cb[n & 1] < bytes;
-      dma16_at(in ? wp[n] + at : zero, buf + kXBytes + (uint32_t)(NWL * wu + n) * 1024u);
+    n -= kXi;
+    if (n < kWi) {
+      const uint32_t to = buf + kXBytes + (uint32_t)(NWL * wu + n) * 1024u;
+      if constexpr (WL == kDma) {
+        const int over = at + cb[n & 1] + 16 - bytes;
+        dma16_at((have >> (16 + n) & 1) && over < 16 ? wp[n] + at - (over > 0 ? over : 0) : zero, to);
+      } else {
+        int64_t k = (int64_t)st * kPer + nw.row0 + n * nw.per;
+        if constexpr (PASS == kDw) k = gathered[n];
+        else if (k >= clen) k = -1;
+        dma16_at(k >= 0 && nw.cb[n & 1] >= 0 ? nw.base + k * nw.stride + nw.cb[n & 1] : zero, to);
+      }
       return;
     }
-    if (WL == kDma) n -= NWL;
+    n -= kWi;
     if constexpr (mx)
       dma4_at(sp && st * kC + n * 4 < bytes / 16 ? sp + st * kC + n * 4 : zero,
               buf + kXBytes + kWBytes + (uint32_t)n * (kXR + kWR) * 4u + (uint32_t)sj * 256u);
@@ -404,6 +490,34 @@ __global__ __launch_bounds__(SH::kThreads, SH::WGS* SH::kThreads / 256) void k_e
   auto issue = [&](int st, int b) {
 #pragma unroll
     for (int n = 0; n < kIssued; ++n) issue_one(st, b, n);
+  };
+
+  // A row's last chunk, where the row ends inside it, has been loaded as the
+  // row's last 16 bytes: once they are there, the lane that loaded them puts them
+  // in place.  (Rows of one contraction index: in every step of the last tile.)
+  const bool ends_x = !mx && XL == kDma && bytes % 16 != 0, ends_w = !mx && WL == kDma && bytes % 16 != 0;
+  const bool edge_x = XL == kNatural && tl.m0 + kXR > a.N && a.N * (int)sizeof(S) % 16 != 0;
+  const bool edge_w = WL == kNatural && n0 + kWR > cols && cols * (int)sizeof(S) % 16 != 0;
+  auto settle = [&](int st, int b) {
+    if constexpr (mx) return;
+    auto move = [&](int at, int drop) {
+      if (drop > 0 && drop < V) {
+        uint4* q = reinterpret_cast<uint4*>(smem + at + lane * 16);
+        *q = without_first<S>(*q, drop);
+      }
+    };
+    const bool last = (st + 1) * kStep > bytes;
+    const int xat = b * kBuf + NXL * wu * 1024, wat = b * kBuf + kXBytes + NWL * wu * 1024;
+    if ((ends_x && last) || edge_x) {
+#pragma unroll
+      for (int n = 0; n < NXL; ++n)
+        move(xat + n * 1024, XL == kNatural ? nx.drop[n & 1] : (st * kStep + cb[n & 1] + 16 - bytes) / (int)sizeof(S));
+    }
+    if ((ends_w && last) || edge_w) {
+#pragma unroll
+      for (int n = 0; n < NWL; ++n)
+        move(wat + n * 1024, WL == kNatural ? nw.drop[n & 1] : (st * kStep + cb[n & 1] + 16 - bytes) / (int)sizeof(S));
+    }
   };
 
   // ---- through registers: step st from memory, and to buffer b
@@ -423,17 +537,20 @@ __global__ __launch_bounds__(SH::kThreads, SH::WGS* SH::kThreads / 256) void k_e
     if constexpr (XL == kGuarded) {
 #pragma unroll
       for (int j = 0; j < NXL; ++j)
-        xg[j] = load_chunk<S>(xp[j] + at, have >> j & 1 ? (bytes - at - cb[j & 1]) / (int)sizeof(S) : 0);
+        xg[j] = load_chunk<S>(xp[j] + at, have >> j & 1 ? (bytes - at - cb[j & 1]) / (int)sizeof(S) : 0,
+                              at + kStep > bytes, bytes >= 16, (const char*)a.x);
     }
     if constexpr (WL == kGuarded) {
 #pragma unroll
       for (int j = 0; j < NWL; ++j)
-        wg[j] = load_chunk<S>(wp[j] + at, have >> (16 + j) & 1 ? (bytes - at - cb[j & 1]) / (int)sizeof(S) : 0);
+        wg[j] = load_chunk<S>(wp[j] + at, have >> (16 + j) & 1 ? (bytes - at - cb[j & 1]) / (int)sizeof(S) : 0,
+                              at + kStep > bytes, bytes >= 16, (const char*)a.w);
     }
     if constexpr (kTr) {
 #pragma unroll
       for (int i = 0; i < V; ++i)
-        sq[i] = load_chunk<S>(sq_p + (sq_row[i] < 0 ? 0 : sq_row[i]) * sq_stride, sq_row[i] < 0 ? 0 : sq_valid);
+        sq[i] = load_chunk<S>(sq_p + (sq_row[i] < 0 ? 0 : sq_row[i]) * sq_stride, sq_row[i] < 0 ? 0 : sq_valid, sq_edge,
+                              sq_wide, sq_x || PASS == kDx ? (const char*)a.w : (const char*)a.x);
     }
   };
   auto put = [&](int b, bool sums) {
@@ -498,7 +615,37 @@ __global__ __launch_bounds__(SH::kThreads, SH::WGS* SH::kThreads / 256) void k_e
   const int tr = turn<kStep>(l32);
   const char* xb = smem + (wm * 32 * MI + l32) * kStep;
   const char* wb = smem + kXBytes + (wn * 32 * NI + l32) * kStep;
+  // the 32 rows (of the tile) from 32 t on, at part h, of an operand in natural order
+  auto read_natural = [&](int from, int tile_rows, int t, int h) -> uint4 {
+    const int tb = tile_rows * (int)sizeof(S);
+    uint4 u;
+    if constexpr (sizeof(S) == 4) {
+      const char* p = smem + from + (8 * h + 4 * lh) * tb + ((t ^ lh) << 7) + l32 * 4;
+      u.x = *reinterpret_cast<const uint32_t*>(p);
+      u.y = *reinterpret_cast<const uint32_t*>(p + tb);
+      u.z = *reinterpret_cast<const uint32_t*>(p + 2 * tb);
+      u.w = *reinterpret_cast<const uint32_t*>(p + 3 * tb);
+    } else {
+      // 16 lanes read 16 columns of four contraction rows, four lanes a row, and
+      // get a column's four values each
+      typedef short s16x4_t __attribute__((ext_vector_type(4)));
+      typedef __attribute__((address_space(3))) s16x4_t* Ptr;
+      const int r = (lane & 15) >> 2, row = 16 * h + 8 * lh + r;
+      const int block = tb == 128 ? t ^ (r >> 1) : t ^ r;
+      const char* p = smem + from + row * tb + (block << 6) + ((lane >> 4) & 1) * 32 + (lane & 3) * 8;
+      const s16x4_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Ptr)p);
+      const s16x4_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Ptr)(p + 4 * tb));
+      const uint2 l2 = __builtin_bit_cast(uint2, lo), h2 = __builtin_bit_cast(uint2, hi);
+      u = make_uint4(l2.x, l2.y, h2.x, h2.y);
+    }
+    return u;
+  };
   auto read_x = [&](int b, int h) {
+    if constexpr (XL == kNatural) {
+#pragma unroll
+      for (int i = 0; i < MI; ++i) fr[h & 1].x[i] = read_natural(b * kBuf, kXR, wm * MI + i, h);
+      return;
+    }
     const int at = b * kBuf + 16 * ((2 * h + lh) ^ tr);
 #pragma unroll
     for (int i = 0; i < MI; ++i) fr[h & 1].x[i] = *reinterpret_cast<const uint4*>(xb + at + 32 * i * kStep);
@@ -514,6 +661,10 @@ __global__ __launch_bounds__(SH::kThreads, SH::WGS* SH::kThreads / 256) void k_e
     }
   };
   auto read_w = [&](int b, int h, int t) {
+    if constexpr (WL == kNatural) {
+      fr[h & 1].w[t] = read_natural(b * kBuf + kXBytes, kWR, wn * NI + t, h);
+      return;
+    }
     const int at = b * kBuf + 16 * ((2 * h + lh) ^ tr);
     fr[h & 1].w[t] = *reinterpret_cast<const uint4*>(wb + at + 32 * t * kStep);
   };
@@ -522,6 +673,18 @@ __global__ __launch_bounds__(SH::kThreads, SH::WGS* SH::kThreads / 256) void k_e
 #pragma unroll
     for (int i = 0; i < MI; ++i)
       acc[i][t] = M::template mma<2 * h>(fr[h].w[t], fr[h].x[i], acc[i][t], sw[0][t], sx[0][i]);
+  };
+  // dw: the sums of dy's columns are one more product, with a row operand of ones
+  constexpr bool kSums = PASS == kDw && XL == kNatural;
+  f32x16_t ones_acc[kSums ? MI : 1];
+  auto mul_ones = [&](auto hc) {
+    if constexpr (kSums) {
+      constexpr int h = decltype(hc)::value;
+      const uint32_t one = sizeof(S) == 4 ? 0x3f800000u : 0x3f803f80u;
+#pragma unroll
+      for (int i = 0; i < MI; ++i)
+        ones_acc[i] = M::template mma<0>(make_uint4(one, one, one, one), fr[h].x[i], ones_acc[i], 0, 0);
+    }
   };
   auto next_scales = [&]() {
     if constexpr (mx) {
@@ -544,6 +707,9 @@ __global__ __launch_bounds__(SH::kThreads, SH::WGS* SH::kThreads / 256) void k_e
   const bool whole = ((cols | (int)(a.out_stride % kEl)) & (kEl - 1)) == 0 && (uintptr_t)a.out % 16 == 0;
 
   const bool sums = PASS == kDw && a.db && tl.nt == 0;
+  const bool ones = kSums && sums && wn == 0;
+#pragma unroll
+  for (int i = 0; i < (kSums ? MI : 1); ++i) ones_acc[i] = zero16();
   float bias = 0.0f;
   if (biased && tid < kWR && n0 + tid < a.N) bias = a.bias[(int64_t)tl.e * a.N + n0 + tid];
 #pragma unroll
@@ -554,6 +720,7 @@ __global__ __launch_bounds__(SH::kThreads, SH::WGS* SH::kThreads / 256) void k_e
     for (int t = 0; t < NI; ++t) acc[i][t] = zero16();
 
   if (nst > 0) {
+    gather(0);
     issue(0, 0);
     if constexpr (!kAllDma) {
       place(0);
@@ -565,9 +732,13 @@ __global__ __launch_bounds__(SH::kThreads, SH::WGS* SH::kThreads / 256) void k_e
         place(2);
       }
     }
-    if (nst > 1) issue(1, 1);
+    if (nst > 1) {
+      gather(1);
+      issue(1, 1);
+    }
     if (nst > 1) wait_vm<kIssued>();
     else wait_vm<0>();
+    settle(0, 0);
     __syncthreads();
     if (has_rows) {
       read_x(0, 0);
@@ -590,7 +761,9 @@ __global__ __launch_bounds__(SH::kThreads, SH::WGS* SH::kThreads / 256) void k_e
           mul(std::integral_constant<int, h & 1>{}, t);
           __builtin_amdgcn_sched_barrier(0);
         }
+        if (ones) mul_ones(std::integral_constant<int, h & 1>{});
       };
+      if (ahead) gather(st + 2);                     // ahead of the loads that go by it
       if (has_rows) {
         part(std::integral_constant<int, 0>{});
         if constexpr (kQ == 4) {
@@ -602,6 +775,7 @@ __global__ __launch_bounds__(SH::kThreads, SH::WGS* SH::kThreads / 256) void k_e
         if (more) put(b ^ 1, sums);
       }
       wait_vm<0>();
+      if (more) settle(st + 1, b ^ 1);
       __syncthreads();
       if constexpr (!kAllDma) {
         if (ahead) {
@@ -610,6 +784,7 @@ __global__ __launch_bounds__(SH::kThreads, SH::WGS* SH::kThreads / 256) void k_e
         }
       }
       if (has_rows && (!mx || filled == kQ)) {
+        if (ones) mul_ones(std::integral_constant<int, 1>{});
         if (more) read_x(b ^ 1, 0);
 #pragma unroll
         for (int t = 0; t < NI; ++t) {
@@ -627,7 +802,15 @@ __global__ __launch_bounds__(SH::kThreads, SH::WGS* SH::kThreads / 256) void k_e
     }
   }
 
-  if constexpr (PASS == kDw) {
+  if constexpr (kSums) {
+    if (ones && has_rows && lane < 32) {
+#pragma unroll
+      for (int i = 0; i < MI; ++i) {
+        const int64_t c = tl.m0 + wm * 32 * MI + 32 * i + l32;
+        if (c < a.N) a.db[(int64_t)tl.e * a.N + c] = ones_acc[i][0];
+      }
+    }
+  } else if constexpr (PASS == kDw) {
     if (sums) {                                    // column sums of dy: the chunk lanes of a square's rows
 #pragma unroll
       for (int v = 0; v < V; ++v)
@@ -688,7 +871,7 @@ __global__ __launch_bounds__(SH::kThreads, SH::WGS* SH::kThreads / 256) void k_e
             if (a.mask) {
               const int64_t mr = placed_row(a.mask_order, a.k, a.mask_rows, tl.s0 + r);
               const char* mp = (const char*)a.mask + (mr < 0 ? 0 : mr) * a.mask_stride + (size_t)c * sizeof(S);
-              const uint4 mu = load_chunk<S>(mp, cols - c);
+              const uint4 mu = load_chunk<S>(mp, cols - c, n0 + kWR > cols, cols >= V, (const char*)a.mask);
               S me[V];
               O oe[kEl];
               static_assert(PASS != kDx || V == kEl, "dx has its input's type");
@@ -763,12 +946,13 @@ __global__ __launch_bounds__(256, 4) void k_expert_few(ExpertArgs a) {
     const char* xrow = (const char*)a.x + xe * a.x_e + (r < 0 ? 0 : r) * a.x_stride + 16 * lk;
     const char* xsrow = mx ? (const char*)a.xs + xe * a.xs_e + (r < 0 ? 0 : r) * a.xs_stride : nullptr;
     f32x4_t acc = {0.0f, 0.0f, 0.0f, 0.0f};
-    auto load = [&](const char* p, bool have, int st) -> uint4 {
+    auto load = [&](const char* p, bool have, int st, const void* safe_p) -> uint4 {
+      const char* safe = (const char*)safe_p;
       const int left = bytes - st * 64 - 16 * lk;
       if constexpr (VEC || mx) {
         return have && left > 0 ? *reinterpret_cast<const uint4*>(p + st * 64) : make_uint4(0, 0, 0, 0);
       } else {
-        return load_chunk<S>(p + st * 64, have ? left / (int)sizeof(S) : 0);
+        return load_chunk<S>(p + st * 64, have ? left / (int)sizeof(S) : 0, st == nst - 1, bytes >= 16, safe);
       }
     };
     constexpr int U = 8;
@@ -794,8 +978,8 @@ __global__ __launch_bounds__(256, 4) void k_expert_few(ExpertArgs a) {
 #pragma unroll
       for (int u = 0; u < U; ++u) {
         const bool in = b + u < st1;
-        fw[u] = load(wrow, in && n < a.N, b + u);
-        fx[u] = load(xrow, in && r >= 0, b + u);
+        fw[u] = load(wrow, in && n < a.N, b + u, a.w);
+        fx[u] = load(xrow, in && r >= 0, b + u, a.x);
         sw[u] = sx[u] = 0;
       }
       if constexpr (mx) {
@@ -871,13 +1055,18 @@ hipError_t tile_shape(const ExpertArgs& a, hipStream_t s) {
   typedef typename Shapes<TY>::Wide Wide;
   typedef typename Shapes<TY>::Mid Mid;
   typedef typename Shapes<TY>::Small Small;
-  const int64_t w = tile_time<Wide>(a, PASS, 10, 10), m = tile_time<Mid>(a, PASS, 13, 20),
-                n = tile_time<Small>(a, PASS, 20, 40);
+  constexpr bool f = TY == kTypeF32;
+  const int64_t w = tile_time<Wide>(a, PASS, 10, 10), m = tile_time<Mid>(a, PASS, f ? 10 : 12, f ? 10 : 20),
+                n = tile_time<Small>(a, PASS, f ? 10 : 16, f ? 10 : 40);
   if (w <= m && w <= n) return tile_go<Wide, TY, PASS, XL, WL, OUT16>(a, most_tiles<Wide>(a, PASS), s);
   if (m <= n) return tile_go<Mid, TY, PASS, XL, WL, OUT16>(a, most_tiles<Mid>(a, PASS), s);
   return tile_go<Small, TY, PASS, XL, WL, OUT16>(a, most_tiles<Small>(a, PASS), s);
 }
 
+// Loads straight to LDS ask for addresses on dwords and rows of 16 bytes.
+bool on_dwords(int64_t row_bytes, const void* p, int64_t a, int64_t b) {
+  return ((uintptr_t)p | (uintptr_t)row_bytes | (uintptr_t)a | (uintptr_t)b) % 4 == 0 && row_bytes >= 16;
+}
 bool aligned16(const void* p, int64_t a, int64_t b, int64_t c) {
   return ((uintptr_t)p | (uintptr_t)a | (uintptr_t)b | (uintptr_t)c) % 16 == 0;
 }
@@ -905,15 +1094,20 @@ hipError_t forward_out(const ExpertArgs& a, hipStream_t s) {
     return vec ? few_go<TY, true, OUT16>(a, segs, s) : few_go<TY, false, OUT16>(a, segs, s);
   }
   if constexpr (TY == kTypeMx4) return tile_shape<TY, kForward, kDma, kDma, OUT16>(a, s);
-  else if (vec) return tile_shape<TY, kForward, kDma, kDma, OUT16>(a, s);
-  else return tile_shape<TY, kForward, kGuarded, kGuarded, OUT16>(a, s);
+  const int64_t row = a.K * (int64_t)sizeof(typename Mm<TY>::S);
+  if constexpr (TY != kTypeMx4) {
+    if (on_dwords(row, a.x, a.x_stride, a.x_e) && on_dwords(row, a.w, a.w_e, a.w_n))
+      return tile_shape<TY, kForward, kDma, kDma, OUT16>(a, s);
+    return tile_shape<TY, kForward, kGuarded, kGuarded, OUT16>(a, s);
+  }
 }
 
 template <ExpertType TY>
 hipError_t dx_go(const ExpertArgs& a, hipStream_t s) {
   constexpr bool o16 = TY == kTypeBf16;
-  if (aligned16(a.x, a.x_stride, 0, a.K * (int64_t)sizeof(typename Mm<TY>::S)))
-    return tile_shape<TY, kDx, kDma, kTransposed, o16>(a, s);
+  const int64_t e = sizeof(typename Mm<TY>::S);
+  const bool rows = on_dwords(a.K * e, a.x, a.x_stride, 0);
+  if (rows && on_dwords(a.N * e, a.w, a.w_e, a.w_n)) return tile_shape<TY, kDx, kDma, kNatural, o16>(a, s);
   return tile_shape<TY, kDx, kGuarded, kTransposed, o16>(a, s);
 }
 
@@ -932,8 +1126,13 @@ hipError_t launch_expert_dx(const ExpertArgs& a, ExpertType type, hipStream_t s)
 }
 
 hipError_t launch_expert_dw(const ExpertArgs& a, ExpertType type, hipStream_t s) {
-  if (type == kTypeF32) return tile_shape<kTypeF32, kDw, kTransposed, kTransposed, false>(a, s);
-  return tile_shape<kTypeBf16, kDw, kTransposed, kTransposed, false>(a, s);
+  const int64_t e = type == kTypeF32 ? 4 : 2;
+  const bool aligned = on_dwords(a.K * e, a.x, a.x_stride, 0) && on_dwords(a.N * e, a.w, a.w_n, 0);
+  if (type == kTypeF32)
+    return aligned ? tile_shape<kTypeF32, kDw, kNatural, kNatural, false>(a, s)
+                   : tile_shape<kTypeF32, kDw, kTransposed, kTransposed, false>(a, s);
+  return aligned ? tile_shape<kTypeBf16, kDw, kNatural, kNatural, false>(a, s)
+                 : tile_shape<kTypeBf16, kDw, kTransposed, kTransposed, false>(a, s);
 }
 
 }  // namespace gevo

@@ -215,6 +215,8 @@ EXPERTS = [
     (300, 2, 3, 257, 96, "bf16", "bf16", None), (300, 2, 4, 260, 50, "f32", "f32", None),
     (500, 1, 2, 300, 137, "bf16", "f32", None), (150, 3, 70, 24, 40, "bf16", "f32", None),
     (400, 4, 130, 33, 16, "f32", "f32", [5, 129]), (260, 2, 9, 512, 256, "bf16", "bf16", [3]),
+    (500, 1, 2, 302, 138, "bf16", "bf16", None), (300, 2, 3, 34, 70, "bf16", "f32", None), (400, 2, 3, 6, 10, "bf16", "f32", None),
+    (300, 1, 2, 3, 2, "f32", "f32", None), (260, 1, 1, 65, 129, "bf16", "f32", None),
     (1500, 2, 4, 10, 784, "f32", "f32", None), (700, 2, 6, 64, 1000, "bf16", "f32", [0, 5]),
 ]
 
