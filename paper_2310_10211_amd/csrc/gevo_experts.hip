@@ -33,7 +33,7 @@ typedef float f32x4_t __attribute__((ext_vector_type(4)));
 //   Mid    128 x 128
 //   Small  64 x 64: products of few tiles, spread over more of the chip
 // Two buffers hold a step in use and one under way.  Steps of 128 bytes read
-// whole cache lines; the squares of transposed fp32 operands allow 64.
+// whole cache lines.
 template <int RM_, int RN_, int MI_, int NI_, int WGS_, int STEP_>
 struct Shape {
   static constexpr int RM = RM_, RN = RN_, MI = MI_, NI = NI_, WGS = WGS_;
@@ -46,7 +46,7 @@ struct Shape {
   static constexpr int kScaleBytes = (kXR + kWR) * (kStep / 16);
 };
 template <ExpertType TY> struct Shapes {
-  typedef Shape<4, 2, 2, 4, 1, TY == kTypeF32 ? 64 : 128> Wide;
+  typedef Shape<4, 2, 2, 4, 1, 128> Wide;
   typedef Shape<2, 2, 2, 2, 3, 64> Mid;
   typedef Shape<2, 2, 1, 1, 4, 128> Small;
 };
@@ -263,7 +263,8 @@ __device__ __forceinline__ uint4 load_chunk(const char* p, int valid, bool edge,
   return valid > 0 ? u : make_uint4(0, 0, 0, 0);
 }
 
-enum Load { kDma, kGuarded, kTransposed, kNatural };
+enum Load { kDma, kGuarded, kNatural, kNaturalGuarded };
+constexpr bool by_index(Load l) { return l == kNatural || l == kNaturalGuarded; }
 enum Pass { kForward, kDx, kDw };
 
 }  // namespace
@@ -276,8 +277,7 @@ enum Pass { kForward, kDx, kDw };
 //                contraction index each, straight to LDS; bf16 operands are read
 //                with gfx950's transposing LDS read (each 16 lanes a 4 x 16 block
 //                by columns), fp32 ones value by value
-//   kTransposed  the same at any address or width: a lane loads a square of
-//                8 x 8 (fp32: 4 x 4) values and turns it in registers
+//   kNaturalGuarded  the same through registers, at any address or width
 template <typename SH, ExpertType TY, Pass PASS, Load XL, Load WL, bool OUT16>
 __global__ __launch_bounds__(SH::kThreads, SH::WGS* SH::kThreads / 256) void k_expert_tile(ExpertArgs a) {
   typedef Mm<TY> M;
@@ -338,26 +338,8 @@ __global__ __launch_bounds__(SH::kThreads, SH::WGS* SH::kThreads / 256) void k_e
   const int sj = wu % kSn;
   static_assert(!mx || SH::kWaves >= kSn, "every row's scales have a wave");
 
-  // ---- transposed: squares of V contraction rows x V columns, one a thread,
-  // the w tile's first.  A square's V chunks are one chunk column of V rows of
-  // the tile.
-  constexpr bool kTr = XL == kTransposed || WL == kTransposed;
-  constexpr int kWsq = WL == kTransposed ? kWR / V * kC : 0, kXsq = XL == kTransposed ? kXR / V * kC : 0;
-  static_assert(kWsq + kXsq <= SH::kThreads, "one square a thread");
-  uint4 sq[kTr ? V : 1];
-  const bool sq_x = tid >= kWsq, sq_live = tid < kWsq + kXsq;
-  const int sq_id = sq_x ? tid - kWsq : tid, sq_kc = sq_id % kC, sq_r0 = sq_id / kC * V;
-  const char* sq_p = nullptr;                        // contraction row 0, the square's first column
-  int64_t sq_stride = 0;
-  int sq_valid = 0;                                  // columns that exist
-  // the tiles' columns: all there; rows of at least 16 bytes
-  const bool sq_edge = n0 + kWR > cols || (PASS == kDw && tl.m0 + kXR > a.N);
-  const bool sq_wide = cols >= V && (PASS != kDw || a.N >= V);
-  int32_t sq_row[kTr ? V : 1];                       // rows of the step to fetch next
-  float dbs[V];
-
   {
-    if constexpr (XL != kTransposed) {
+    if constexpr (XL == kDma || XL == kGuarded) {
 #pragma unroll
       for (int j = 0; j < NXL; ++j) {
         const int64_t i = tl.m0 + kLR * (NXL * wave + j) + crow;
@@ -367,7 +349,7 @@ __global__ __launch_bounds__(SH::kThreads, SH::WGS* SH::kThreads / 256) void k_e
         xp[j] = (const char*)a.x + (a.offsets ? 0 : tl.e * a.x_e) + r * a.x_stride + cb[j & 1];
       }
     }
-    if constexpr (WL != kTransposed) {
+    if constexpr (WL == kDma || WL == kGuarded) {
 #pragma unroll
       for (int j = 0; j < NWL; ++j) {
         const int n = n0 + kLR * (NWL * wave + j) + crow;
@@ -386,24 +368,6 @@ __global__ __launch_bounds__(SH::kThreads, SH::WGS* SH::kThreads / 256) void k_e
         if (n < a.N) sp = (const char*)a.ws + tl.e * a.ws_e + n * a.ws_n;
       }
     }
-    if constexpr (kTr) {
-      const int c = (PASS == kDw && sq_x ? (int)tl.m0 : n0) + sq_r0;
-      if (PASS == kDx) {                             // columns of W_e, contraction over its rows
-        sq_p = (const char*)a.w + tl.e * a.w_e;
-        sq_stride = a.w_n;
-        sq_valid = a.N - c;
-      } else if (sq_x) {                             // dw: columns of dy
-        sq_p = (const char*)a.w + tl.s0 * a.w_n;
-        sq_stride = a.w_n;
-        sq_valid = a.N - c;
-      } else {                                       // dw: columns of x, gathered rows
-        sq_p = (const char*)a.x;
-        sq_stride = a.x_stride;
-        sq_valid = a.K - c;
-      }
-      if (!sq_live || sq_valid < 0) sq_valid = 0;
-      sq_p += (size_t)c * sizeof(S);
-    }
   }
 
   // ---- natural order: a load's 1,024 bytes are 1,024 / kRowBytes rows of one
@@ -415,13 +379,14 @@ __global__ __launch_bounds__(SH::kThreads, SH::WGS* SH::kThreads / 256) void k_e
     int64_t stride;
     int row0, per;                                   // the lane's row in the wave's first load; rows a load
     int cb[2];                                       // its column's byte in even and odd loads, -1: none
-    int drop[2];                                     // elements of the chunk before that column
+    int drop[2], valid[2];                           // elements of the chunk before that column; that exist
   } nx{}, nw{};
   auto natural_block = [](int tile_bytes, int row) {  // what the row's 16-byte chunks are xored with
     if (sizeof(S) == 4) return ((row >> 2) & 1) << 3;
     return (tile_bytes == 128 ? (row >> 1) & 1 : row & 3) << 2;
   };
-  auto natural_setup = [&](Natural& d, const char* base, int64_t stride, int tile_rows, int loads, int col0, int width) {
+  auto natural_setup = [&](Natural& d, const char* base, int64_t stride, int tile_rows, int loads, int col0, int width,
+                           bool guarded) {
     const int tb = tile_rows * (int)sizeof(S);       // bytes of a tile's row
     d.base = base;
     d.stride = stride;
@@ -433,18 +398,19 @@ __global__ __launch_bounds__(SH::kThreads, SH::WGS* SH::kThreads / 256) void k_e
       const int c = col0 * (int)sizeof(S) + 16 * ch;
       const int over = c + 16 - width * (int)sizeof(S);   // as below
       d.drop[v] = over > 0 && over < 16 ? over / (int)sizeof(S) : 0;
-      d.cb[v] = over < 16 ? c - (over > 0 ? over : 0) : -1;
+      d.valid[v] = over < 16 ? V - (over > 0 ? over / (int)sizeof(S) : 0) : 0;
+      d.cb[v] = over >= 16 ? -1 : guarded ? c : c - (over > 0 ? over : 0);
     }
   };
-  if constexpr (XL == kNatural)                      // dw: columns of dy
-    natural_setup(nx, (const char*)a.w + tl.s0 * a.w_n, a.w_n, kXR, NXL, (int)tl.m0, a.N);
-  if constexpr (WL == kNatural) {
-    if constexpr (PASS == kDw) natural_setup(nw, (const char*)a.x, a.x_stride, kWR, NWL, n0, a.K);
-    else natural_setup(nw, (const char*)a.w + tl.e * a.w_e, a.w_n, kWR, NWL, n0, a.N);
+  if constexpr (by_index(XL))                        // dw: columns of dy
+    natural_setup(nx, (const char*)a.w + tl.s0 * a.w_n, a.w_n, kXR, NXL, (int)tl.m0, a.N, XL != kNatural);
+  if constexpr (by_index(WL)) {
+    if constexpr (PASS == kDw) natural_setup(nw, (const char*)a.x, a.x_stride, kWR, NWL, n0, a.K, WL != kNatural);
+    else natural_setup(nw, (const char*)a.w + tl.e * a.w_e, a.w_n, kWR, NWL, n0, a.N, WL != kNatural);
   }
-  int32_t gathered[PASS == kDw && WL == kNatural ? NWL : 1];   // rows of x that the next step's loads read
+  int32_t gathered[PASS == kDw ? NWL : 1];   // rows of x that the next step's loads read
   auto gather = [&](int st) {
-    if constexpr (PASS == kDw && WL == kNatural) {
+    if constexpr (PASS == kDw) {
 #pragma unroll
       for (int n = 0; n < NWL; ++n) {
         const int64_t k = (int64_t)st * kPer + nw.row0 + n * nw.per;
@@ -521,74 +487,54 @@ __global__ __launch_bounds__(SH::kThreads, SH::WGS* SH::kThreads / 256) void k_e
   };
 
   // ---- through registers: step st from memory, and to buffer b
-  uint4 xg[XL == kGuarded ? NXL : 1], wg[WL == kGuarded ? NWL : 1];
-  auto place = [&](int st) {                         // rows of a step's squares
-    if constexpr (kTr) {
-#pragma unroll
-      for (int i = 0; i < V; ++i) {
-        const int k = st * kPer + sq_kc * V + i;
-        sq_row[i] = k < clen && sq_valid > 0 ? k : -1;
-        if (PASS == kDw && !sq_x && sq_row[i] >= 0) sq_row[i] = (int)source_row(a, tl.s0, k);
-      }
-    }
-  };
+  constexpr bool kXg = XL == kGuarded || XL == kNaturalGuarded, kWg = WL == kGuarded || WL == kNaturalGuarded;
+  uint4 xg[kXg ? NXL : 1], wg[kWg ? NWL : 1];
+  const bool nat_edge = n0 + kWR > cols || (PASS == kDw && tl.m0 + kXR > a.N);   // some chunk may be partly filled
   auto fetch = [&](int st) {
     const int at = st * kStep;
-    if constexpr (XL == kGuarded) {
+    auto by_row = [&](const char* p, bool in, int n, const void* safe) {
+      return load_chunk<S>(p + at, in ? (bytes - at - cb[n & 1]) / (int)sizeof(S) : 0, at + kStep > bytes, bytes >= 16,
+                           (const char*)safe);
+    };
+    auto by_column = [&](const Natural& d, int64_t k, int n, int width, const void* safe) {
+      const bool in = k >= 0 && d.cb[n & 1] >= 0;
+      return load_chunk<S>(d.base + (in ? k * d.stride + d.cb[n & 1] : 0), in ? d.valid[n & 1] : 0, nat_edge, width >= V,
+                           (const char*)safe);
+    };
+    if constexpr (kXg) {
 #pragma unroll
-      for (int j = 0; j < NXL; ++j)
-        xg[j] = load_chunk<S>(xp[j] + at, have >> j & 1 ? (bytes - at - cb[j & 1]) / (int)sizeof(S) : 0,
-                              at + kStep > bytes, bytes >= 16, (const char*)a.x);
-    }
-    if constexpr (WL == kGuarded) {
-#pragma unroll
-      for (int j = 0; j < NWL; ++j)
-        wg[j] = load_chunk<S>(wp[j] + at, have >> (16 + j) & 1 ? (bytes - at - cb[j & 1]) / (int)sizeof(S) : 0,
-                              at + kStep > bytes, bytes >= 16, (const char*)a.w);
-    }
-    if constexpr (kTr) {
-#pragma unroll
-      for (int i = 0; i < V; ++i)
-        sq[i] = load_chunk<S>(sq_p + (sq_row[i] < 0 ? 0 : sq_row[i]) * sq_stride, sq_row[i] < 0 ? 0 : sq_valid, sq_edge,
-                              sq_wide, sq_x || PASS == kDx ? (const char*)a.w : (const char*)a.x);
-    }
-  };
-  auto put = [&](int b, bool sums) {
-    char* buf = smem + b * kBuf;
-    if constexpr (XL == kGuarded) {
-#pragma unroll
-      for (int j = 0; j < NXL; ++j) *reinterpret_cast<uint4*>(buf + (NXL * wave + j) * 1024 + lane * 16) = xg[j];
-    }
-    if constexpr (WL == kGuarded) {
-#pragma unroll
-      for (int j = 0; j < NWL; ++j)
-        *reinterpret_cast<uint4*>(buf + kXBytes + (NWL * wave + j) * 1024 + lane * 16) = wg[j];
-    }
-    if constexpr (kTr) {
-      if (!sq_live) return;
-      if (!sq_x) buf += kXBytes;
-#pragma unroll
-      for (int c = 0; c < V; ++c) {
-        uint4 o;
-        if constexpr (V == 8) {
-          uint32_t w[4];
-#pragma unroll
-          for (int p = 0; p < 4; ++p) {              // values c of contraction rows 2p, 2p + 1
-            const uint32_t lo = (&sq[2 * p].x)[c >> 1], hi = (&sq[2 * p + 1].x)[c >> 1];
-            w[p] = __builtin_amdgcn_perm(hi, lo, c & 1 ? 0x07060302u : 0x05040100u);
-          }
-          o = make_uint4(w[0], w[1], w[2], w[3]);
+      for (int n = 0; n < NXL; ++n) {
+        if constexpr (XL == kGuarded) {
+          xg[n] = by_row(xp[n], have >> n & 1, n, a.x);
         } else {
-          o = make_uint4((&sq[0].x)[c], (&sq[1].x)[c], (&sq[2].x)[c], (&sq[3].x)[c]);
-        }
-        *reinterpret_cast<uint4*>(buf + (sq_r0 + c) * kStep + 16 * (sq_kc ^ turn<kStep>(sq_r0 + c))) = o;
-        if (PASS == kDw && sq_x && sums) {
-          S e[V];
-          __builtin_memcpy(e, &o, 16);
-#pragma unroll
-          for (int i = 0; i < V; ++i) dbs[c] += Op<S>::to_f32(e[i]);
+          const int64_t k = (int64_t)st * kPer + nx.row0 + n * nx.per;
+          xg[n] = by_column(nx, k < clen ? k : -1, n, a.N, a.w);
         }
       }
+    }
+    if constexpr (kWg) {
+#pragma unroll
+      for (int n = 0; n < NWL; ++n) {
+        if constexpr (WL == kGuarded) {
+          wg[n] = by_row(wp[n], have >> (16 + n) & 1, n, a.w);
+        } else {
+          int64_t k = (int64_t)st * kPer + nw.row0 + n * nw.per;
+          if constexpr (PASS == kDw) k = gathered[n];
+          else if (k >= clen) k = -1;
+          wg[n] = by_column(nw, k, n, cols, PASS == kDw ? a.x : a.w);
+        }
+      }
+    }
+  };
+  auto put = [&](int b) {
+    char* buf = smem + b * kBuf + lane * 16;
+    if constexpr (kXg) {
+#pragma unroll
+      for (int n = 0; n < NXL; ++n) *reinterpret_cast<uint4*>(buf + (NXL * wave + n) * 1024) = xg[n];
+    }
+    if constexpr (kWg) {
+#pragma unroll
+      for (int n = 0; n < NWL; ++n) *reinterpret_cast<uint4*>(buf + kXBytes + (NWL * wave + n) * 1024) = wg[n];
     }
   };
 
@@ -641,7 +587,7 @@ __global__ __launch_bounds__(SH::kThreads, SH::WGS* SH::kThreads / 256) void k_e
     return u;
   };
   auto read_x = [&](int b, int h) {
-    if constexpr (XL == kNatural) {
+    if constexpr (by_index(XL)) {
 #pragma unroll
       for (int i = 0; i < MI; ++i) fr[h & 1].x[i] = read_natural(b * kBuf, kXR, wm * MI + i, h);
       return;
@@ -661,7 +607,7 @@ __global__ __launch_bounds__(SH::kThreads, SH::WGS* SH::kThreads / 256) void k_e
     }
   };
   auto read_w = [&](int b, int h, int t) {
-    if constexpr (WL == kNatural) {
+    if constexpr (by_index(WL)) {
       fr[h & 1].w[t] = read_natural(b * kBuf + kXBytes, kWR, wn * NI + t, h);
       return;
     }
@@ -674,16 +620,18 @@ __global__ __launch_bounds__(SH::kThreads, SH::WGS* SH::kThreads / 256) void k_e
     for (int i = 0; i < MI; ++i)
       acc[i][t] = M::template mma<2 * h>(fr[h].w[t], fr[h].x[i], acc[i][t], sw[0][t], sx[0][i]);
   };
-  // dw: the sums of dy's columns are one more product, with a row operand of ones
-  constexpr bool kSums = PASS == kDw && XL == kNatural;
-  f32x16_t ones_acc[kSums ? MI : 1];
-  auto mul_ones = [&](auto hc) {
+  // dw: sums of dy's columns, a lane's share of its row of the x operand
+  constexpr bool kSums = PASS == kDw;
+  float col_sum[kSums ? MI : 1];
+  auto add_columns = [&](int h) {
     if constexpr (kSums) {
-      constexpr int h = decltype(hc)::value;
-      const uint32_t one = sizeof(S) == 4 ? 0x3f800000u : 0x3f803f80u;
 #pragma unroll
-      for (int i = 0; i < MI; ++i)
-        ones_acc[i] = M::template mma<0>(make_uint4(one, one, one, one), fr[h].x[i], ones_acc[i], 0, 0);
+      for (int i = 0; i < MI; ++i) {
+        S e[V];
+        __builtin_memcpy(e, &fr[h].x[i], 16);
+#pragma unroll
+        for (int v = 0; v < V; ++v) col_sum[i] += Op<S>::to_f32(e[v]);
+      }
     }
   };
   auto next_scales = [&]() {
@@ -707,13 +655,11 @@ __global__ __launch_bounds__(SH::kThreads, SH::WGS* SH::kThreads / 256) void k_e
   const bool whole = ((cols | (int)(a.out_stride % kEl)) & (kEl - 1)) == 0 && (uintptr_t)a.out % 16 == 0;
 
   const bool sums = PASS == kDw && a.db && tl.nt == 0;
-  const bool ones = kSums && sums && wn == 0;
+  const bool adds = kSums && sums && wn == 0;
 #pragma unroll
-  for (int i = 0; i < (kSums ? MI : 1); ++i) ones_acc[i] = zero16();
+  for (int i = 0; i < (kSums ? MI : 1); ++i) col_sum[i] = 0.0f;
   float bias = 0.0f;
   if (biased && tid < kWR && n0 + tid < a.N) bias = a.bias[(int64_t)tl.e * a.N + n0 + tid];
-#pragma unroll
-  for (int v = 0; v < V; ++v) dbs[v] = 0.0f;
 #pragma unroll
   for (int i = 0; i < MI; ++i)
 #pragma unroll
@@ -723,17 +669,12 @@ __global__ __launch_bounds__(SH::kThreads, SH::WGS* SH::kThreads / 256) void k_e
     gather(0);
     issue(0, 0);
     if constexpr (!kAllDma) {
-      place(0);
       fetch(0);
-      place(1);
-      put(0, sums);
-      if (nst > 1) {
-        fetch(1);
-        place(2);
-      }
+      put(0);
     }
     if (nst > 1) {
       gather(1);
+      if constexpr (!kAllDma) fetch(1);
       issue(1, 1);
     }
     if (nst > 1) wait_vm<kIssued>();
@@ -761,7 +702,7 @@ __global__ __launch_bounds__(SH::kThreads, SH::WGS* SH::kThreads / 256) void k_e
           mul(std::integral_constant<int, h & 1>{}, t);
           __builtin_amdgcn_sched_barrier(0);
         }
-        if (ones) mul_ones(std::integral_constant<int, h & 1>{});
+        if (adds) add_columns(h & 1);
       };
       if (ahead) gather(st + 2);                     // ahead of the loads that go by it
       if (has_rows) {
@@ -772,19 +713,16 @@ __global__ __launch_bounds__(SH::kThreads, SH::WGS* SH::kThreads / 256) void k_e
         }
       }
       if constexpr (!kAllDma) {
-        if (more) put(b ^ 1, sums);
+        if (more) put(b ^ 1);
       }
       wait_vm<0>();
       if (more) settle(st + 1, b ^ 1);
       __syncthreads();
       if constexpr (!kAllDma) {
-        if (ahead) {
-          fetch(st + 2);
-          place(st + 3);
-        }
+        if (ahead) fetch(st + 2);
       }
       if (has_rows && (!mx || filled == kQ)) {
-        if (ones) mul_ones(std::integral_constant<int, 1>{});
+        if (adds) add_columns(1);
         if (more) read_x(b ^ 1, 0);
 #pragma unroll
         for (int t = 0; t < NI; ++t) {
@@ -803,24 +741,12 @@ __global__ __launch_bounds__(SH::kThreads, SH::WGS* SH::kThreads / 256) void k_e
   }
 
   if constexpr (kSums) {
-    if (ones && has_rows && lane < 32) {
+    if (adds && has_rows) {
 #pragma unroll
       for (int i = 0; i < MI; ++i) {
+        const float sum = col_sum[i] + __shfl_xor(col_sum[i], 32, 64);
         const int64_t c = tl.m0 + wm * 32 * MI + 32 * i + l32;
-        if (c < a.N) a.db[(int64_t)tl.e * a.N + c] = ones_acc[i][0];
-      }
-    }
-  } else if constexpr (PASS == kDw) {
-    if (sums) {                                    // column sums of dy: the chunk lanes of a square's rows
-#pragma unroll
-      for (int v = 0; v < V; ++v)
-#pragma unroll
-        for (int m = 1; m < kC; m <<= 1) dbs[v] += __shfl_xor(dbs[v], m, 64);
-      if (sq_live && sq_x && sq_kc == 0) {
-        const int c = (int)tl.m0 + sq_r0;
-#pragma unroll
-        for (int v = 0; v < V; ++v)
-          if (c + v < a.N) a.db[(int64_t)tl.e * a.N + c + v] = dbs[v];
+        if (lh == 0 && c < a.N) a.db[(int64_t)tl.e * a.N + c] = sum;
       }
     }
   }
@@ -906,7 +832,7 @@ __global__ __launch_bounds__(SH::kThreads, SH::WGS* SH::kThreads / 256) void k_e
 // operand is up to 16 rows of x.  SPLIT: the four waves of a workgroup share 16
 // columns and split their contraction, and their sums are joined in LDS in the
 // waves' order.
-template <ExpertType TY, bool VEC, bool OUT16, bool SPLIT>
+template <ExpertType TY, bool OUT16, bool SPLIT>
 __global__ __launch_bounds__(256, 4) void k_expert_few(ExpertArgs a) {
   typedef Mm<TY> M;
   typedef typename M::S S;
@@ -946,13 +872,18 @@ __global__ __launch_bounds__(256, 4) void k_expert_few(ExpertArgs a) {
     const char* xrow = (const char*)a.x + xe * a.x_e + (r < 0 ? 0 : r) * a.x_stride + 16 * lk;
     const char* xsrow = mx ? (const char*)a.xs + xe * a.xs_e + (r < 0 ? 0 : r) * a.xs_stride : nullptr;
     f32x4_t acc = {0.0f, 0.0f, 0.0f, 0.0f};
-    auto load = [&](const char* p, bool have, int st, const void* safe_p) -> uint4 {
-      const char* safe = (const char*)safe_p;
-      const int left = bytes - st * 64 - 16 * lk;
-      if constexpr (VEC || mx) {
+    // a chunk of step st; whole: the step lies inside the row
+    auto load = [&](const char* p, bool have, int st, const void* safe, bool whole) -> uint4 {
+      uint4 u;
+      if (whole) {
+        __builtin_memcpy(&u, p + st * 64, 16);       // (an absent row's pointer is row 0's)
+        return have ? u : make_uint4(0, 0, 0, 0);
+      }
+      const int left = st < st1 ? bytes - st * 64 - 16 * lk : 0;
+      if constexpr (mx) {
         return have && left > 0 ? *reinterpret_cast<const uint4*>(p + st * 64) : make_uint4(0, 0, 0, 0);
       } else {
-        return load_chunk<S>(p + st * 64, have ? left / (int)sizeof(S) : 0, st == nst - 1, bytes >= 16, safe);
+        return load_chunk<S>(p + st * 64, have ? left / (int)sizeof(S) : 0, true, bytes >= 16, (const char*)safe);
       }
     };
     constexpr int U = 8;
@@ -972,14 +903,13 @@ __global__ __launch_bounds__(256, 4) void k_expert_few(ExpertArgs a) {
         for (int d = 0; d < 4; ++d) v[u + d] = q[d] >> (8 * lk);
       }
     };
-    for (int b = st0; b < st1; b += U) {
+    auto group = [&](int b, auto whole) {
       uint4 fw[U], fx[U];
       uint32_t sw[U], sx[U];
 #pragma unroll
       for (int u = 0; u < U; ++u) {
-        const bool in = b + u < st1;
-        fw[u] = load(wrow, in && n < a.N, b + u, a.w);
-        fx[u] = load(xrow, in && r >= 0, b + u, a.x);
+        fw[u] = load(wrow, n < a.N, b + u, a.w, decltype(whole)::value);
+        fx[u] = load(xrow, r >= 0, b + u, a.x, decltype(whole)::value);
         sw[u] = sx[u] = 0;
       }
       if constexpr (mx) {
@@ -988,7 +918,10 @@ __global__ __launch_bounds__(256, 4) void k_expert_few(ExpertArgs a) {
       }
 #pragma unroll
       for (int u = 0; u < U; ++u) acc = M::mma16(fw[u], fx[u], acc, sw[u], sx[u]);
-    }
+    };
+    int b = st0;
+    for (; b + U <= st1 && (b + U) * 64 <= bytes; b += U) group(b, std::true_type{});
+    for (; b < st1; b += U) group(b, std::false_type{});
     if constexpr (SPLIT) {
       __syncthreads();                               // the last tile's sums have been read
       part[wave][lane] = acc;
@@ -1067,31 +1000,28 @@ hipError_t tile_shape(const ExpertArgs& a, hipStream_t s) {
 bool on_dwords(int64_t row_bytes, const void* p, int64_t a, int64_t b) {
   return ((uintptr_t)p | (uintptr_t)row_bytes | (uintptr_t)a | (uintptr_t)b) % 4 == 0 && row_bytes >= 16;
 }
-bool aligned16(const void* p, int64_t a, int64_t b, int64_t c) {
-  return ((uintptr_t)p | (uintptr_t)a | (uintptr_t)b | (uintptr_t)c) % 16 == 0;
-}
-
 // The contraction is split where 16 columns a wave would leave the chip less
 // than eight waves a CU, if each of its parts is a few loads long.
-template <ExpertType TY, bool VEC, bool OUT16>
+template <ExpertType TY, bool OUT16>
 hipError_t few_go(const ExpertArgs& a, int64_t segs, hipStream_t s) {
   const int64_t bands = (a.N + 15) / 16;
   const int64_t bytes = TY == kTypeMx4 ? (a.K + 127) / 128 * 64 : a.K * (int64_t)sizeof(typename Mm<TY>::S);
   if (bands * segs < 2048 && bytes >= 1024)
-    k_expert_few<TY, VEC, OUT16, true><<<dim3((unsigned)bands, (unsigned)segs), 256, 0, s>>>(a);
+    k_expert_few<TY, OUT16, true><<<dim3((unsigned)bands, (unsigned)segs), 256, 0, s>>>(a);
   else
-    k_expert_few<TY, VEC, OUT16, false><<<dim3((unsigned)((bands + 3) / 4), (unsigned)segs), 256, 0, s>>>(a);
+    k_expert_few<TY, OUT16, false><<<dim3((unsigned)((bands + 3) / 4), (unsigned)segs), 256, 0, s>>>(a);
   return hipGetLastError();
 }
 
 template <ExpertType TY, bool OUT16>
 hipError_t forward_out(const ExpertArgs& a, hipStream_t s) {
-  const bool vec = TY == kTypeMx4 || (aligned16(a.x, a.x_stride, a.x_e, a.K * (int64_t)sizeof(typename Mm<TY>::S)) &&
-                                      aligned16(a.w, a.w_e, a.w_n, 0));
-  // Up to 16 rows a segment on average the weights' bytes bound the product
+  // Up to 16 rows a segment on average the weights' bytes bound the product; up
+  // to 64, where tiles would leave CUs idle, reading them again for every 16 rows
+  // costs less than long contractions on a few CUs (81 rows over 3 experts of
+  // 1062 x 2611 in fp32: 32 us, tiles 70).
   const int64_t segs = a.offsets ? (a.S < a.E ? a.S : a.E) : a.E;
-  if (a.S <= segs * 16 && segs <= 65535) {
-    return vec ? few_go<TY, true, OUT16>(a, segs, s) : few_go<TY, false, OUT16>(a, segs, s);
+  if (segs <= 65535 && (a.S <= segs * 16 || (a.S <= segs * 64 && most_tiles<typename Shapes<TY>::Small>(a, kForward) < 256))) {
+    return few_go<TY, OUT16>(a, segs, s);
   }
   if constexpr (TY == kTypeMx4) return tile_shape<TY, kForward, kDma, kDma, OUT16>(a, s);
   const int64_t row = a.K * (int64_t)sizeof(typename Mm<TY>::S);
@@ -1108,7 +1038,7 @@ hipError_t dx_go(const ExpertArgs& a, hipStream_t s) {
   const int64_t e = sizeof(typename Mm<TY>::S);
   const bool rows = on_dwords(a.K * e, a.x, a.x_stride, 0);
   if (rows && on_dwords(a.N * e, a.w, a.w_e, a.w_n)) return tile_shape<TY, kDx, kDma, kNatural, o16>(a, s);
-  return tile_shape<TY, kDx, kGuarded, kTransposed, o16>(a, s);
+  return tile_shape<TY, kDx, kGuarded, kNaturalGuarded, o16>(a, s);
 }
 
 }  // namespace
@@ -1130,9 +1060,9 @@ hipError_t launch_expert_dw(const ExpertArgs& a, ExpertType type, hipStream_t s)
   const bool aligned = on_dwords(a.K * e, a.x, a.x_stride, 0) && on_dwords(a.N * e, a.w, a.w_n, 0);
   if (type == kTypeF32)
     return aligned ? tile_shape<kTypeF32, kDw, kNatural, kNatural, false>(a, s)
-                   : tile_shape<kTypeF32, kDw, kTransposed, kTransposed, false>(a, s);
+                   : tile_shape<kTypeF32, kDw, kNaturalGuarded, kNaturalGuarded, false>(a, s);
   return aligned ? tile_shape<kTypeBf16, kDw, kNatural, kNatural, false>(a, s)
-                 : tile_shape<kTypeBf16, kDw, kTransposed, kTransposed, false>(a, s);
+                 : tile_shape<kTypeBf16, kDw, kNaturalGuarded, kNaturalGuarded, false>(a, s);
 }
 
 }  // namespace gevo

@@ -587,36 +587,49 @@ namespace {
 
 template <typename S, int V> struct Vec;
 template <> struct Vec<float, 4> { typedef float4 T; };
-template <> struct Vec<float, 1> { typedef float T; };
 template <> struct Vec<uint16_t, 4> { typedef uint2 T; };
 template <> struct Vec<uint16_t, 8> { typedef uint4 T; };
-template <> struct Vec<uint16_t, 1> { typedef uint16_t T; };
 
-template <typename S, int V>
-__device__ __forceinline__ void load_f(const S* p, float (&f)[V]) {
-  typedef typename Vec<S, V>::T T;
-  T v = *reinterpret_cast<const T*>(p);
+// V elements at p, of which `valid` exist.  WHOLE: all of them, aligned; else one
+// load or store at any address, or element by element at a row's end.
+template <typename S, int V, bool WHOLE>
+__device__ __forceinline__ void load_f(const S* p, int valid, float (&f)[V]) {
   S e[V];
-  __builtin_memcpy(e, &v, sizeof(v));
+  if (WHOLE) {
+    typename Vec<S, V>::T v = *reinterpret_cast<const typename Vec<S, V>::T*>(p);
+    __builtin_memcpy(e, &v, sizeof(e));
+  } else if (valid >= V) {
+    __builtin_memcpy(e, p, sizeof(e));
+  } else {
+#pragma unroll
+    for (int i = 0; i < V; ++i) e[i] = i < valid ? p[i] : (S)0;
+  }
 #pragma unroll
   for (int i = 0; i < V; ++i) f[i] = to_f<S>(e[i]);
 }
-template <typename S, int V>
-__device__ __forceinline__ void store_f(S* p, const float (&f)[V]) {
-  typedef typename Vec<S, V>::T T;
+template <typename S, int V, bool WHOLE>
+__device__ __forceinline__ void store_f(S* p, int valid, const float (&f)[V]) {
   S e[V];
 #pragma unroll
   for (int i = 0; i < V; ++i) e[i] = from_f<S>(f[i]);
-  T v;
-  __builtin_memcpy(&v, e, sizeof(v));
-  *reinterpret_cast<T*>(p) = v;
+  if (WHOLE) {
+    typename Vec<S, V>::T v;
+    __builtin_memcpy(&v, e, sizeof(v));
+    *reinterpret_cast<typename Vec<S, V>::T*>(p) = v;
+  } else if (valid >= V) {
+    __builtin_memcpy(p, e, sizeof(e));
+  } else {
+#pragma unroll
+    for (int i = 0; i < V; ++i)
+      if (i < valid) p[i] = e[i];
+  }
 }
 
 }  // namespace
 
 // y[t] = sum_j w[t][j] rows[pos[t][j]], summed in j's order in 32 bits and
 // rounded once; a slot without a row adds w 0.  A thread takes V columns of a row t.
-template <typename S, typename O, int V>
+template <typename S, typename O, int V, bool WHOLE>
 __global__ __launch_bounds__(256) void k_combine(CombineArgs a, int cols, int64_t total) {
   const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
   if (i >= total) return;
@@ -633,7 +646,7 @@ __global__ __launch_bounds__(256) void k_combine(CombineArgs a, int cols, int64_
     const float wj = w ? w[j] : 1.0f;
     float x[V];
     if (p >= 0) {
-      load_f<S, V>((const S*)a.rows + (int64_t)p * a.rows_stride + c, x);
+      load_f<S, V, WHOLE>((const S*)a.rows + (int64_t)p * a.rows_stride + c, a.N - c, x);
     } else {
 #pragma unroll
       for (int v = 0; v < V; ++v) x[v] = 0.0f;
@@ -641,12 +654,12 @@ __global__ __launch_bounds__(256) void k_combine(CombineArgs a, int cols, int64_
 #pragma unroll
     for (int v = 0; v < V; ++v) acc[v] = fmaf(wj, x[v], acc[v]);
   }
-  store_f<O, V>((O*)a.y + t * a.y_stride + c, acc);
+  store_f<O, V, WHOLE>((O*)a.y + t * a.y_stride + c, a.N - c, acc);
 }
 
 // Slot (t, j): drows[pos] = w dy[t], dweights[t][j] = sum_n dy[t][n] rows[pos][n].
 // One wave per slot; the slots of a row follow each other, so dy comes from the caches.
-template <typename S, int V>
+template <typename S, int V, bool WHOLE>
 __global__ __launch_bounds__(256) void k_combine_bwd(CombineArgs a) {
   const int lane = threadIdx.x & 63;
   const int64_t slot = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
@@ -662,16 +675,16 @@ __global__ __launch_bounds__(256) void k_combine_bwd(CombineArgs a) {
 #pragma unroll 2
     for (int c = lane * V; c < a.N; c += 64 * V) {
       float d[V], x[V];
-      load_f<S, V>(dy + c, d);
+      load_f<S, V, WHOLE>(dy + c, a.N - c, d);
       if (a.dweights) {
-        load_f<S, V>(row + c, x);
+        load_f<S, V, WHOLE>(row + c, a.N - c, x);
 #pragma unroll
         for (int v = 0; v < V; ++v) dot = fmaf(d[v], x[v], dot);
       }
       if (a.drows) {
 #pragma unroll
         for (int v = 0; v < V; ++v) x[v] = w * d[v];
-        store_f<S, V>(drow + c, x);
+        store_f<S, V, WHOLE>(drow + c, a.N - c, x);
       }
     }
   }
@@ -688,12 +701,12 @@ bool vec_ok(const void* p, int64_t stride, int N, int V, size_t elt) {
 
 template <typename S, typename O>
 hipError_t launch_combine(const CombineArgs& a, hipStream_t s) {
-  const bool v4 = vec_ok(a.rows, a.rows_stride, a.N, 4, sizeof(S)) && vec_ok(a.y, a.y_stride, a.N, 4, sizeof(O));
-  const int cols = v4 ? a.N / 4 : a.N;
+  const bool whole = vec_ok(a.rows, a.rows_stride, a.N, 4, sizeof(S)) && vec_ok(a.y, a.y_stride, a.N, 4, sizeof(O));
+  const int cols = (a.N + 3) / 4;
   const int64_t total = a.T * cols, grid = (total + 255) / 256;
   if (grid > 0x7fffffff) return hipErrorInvalidValue;
-  if (v4) k_combine<S, O, 4><<<(unsigned)grid, 256, 0, s>>>(a, cols, total);
-  else k_combine<S, O, 1><<<(unsigned)grid, 256, 0, s>>>(a, cols, total);
+  if (whole) k_combine<S, O, 4, true><<<(unsigned)grid, 256, 0, s>>>(a, cols, total);
+  else k_combine<S, O, 4, false><<<(unsigned)grid, 256, 0, s>>>(a, cols, total);
   return hipGetLastError();
 }
 template hipError_t launch_combine<float, float>(const CombineArgs&, hipStream_t);
@@ -709,8 +722,8 @@ hipError_t launch_combine_backward(const CombineArgs& a, hipStream_t s) {
   const bool vec = vec_ok(a.y, a.y_stride, a.N, V, sizeof(S)) &&
                    (!a.dweights || vec_ok(a.rows, a.rows_stride, a.N, V, sizeof(S))) &&
                    (!a.drows || vec_ok(a.drows, a.N, a.N, V, sizeof(S)));
-  if (vec) k_combine_bwd<S, V><<<(unsigned)grid, 256, 0, s>>>(a);
-  else k_combine_bwd<S, 1><<<(unsigned)grid, 256, 0, s>>>(a);
+  if (vec) k_combine_bwd<S, V, true><<<(unsigned)grid, 256, 0, s>>>(a);
+  else k_combine_bwd<S, V, false><<<(unsigned)grid, 256, 0, s>>>(a);
   return hipGetLastError();
 }
 template hipError_t launch_combine_backward<float>(const CombineArgs&, hipStream_t);
