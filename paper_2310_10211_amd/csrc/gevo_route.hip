@@ -113,15 +113,21 @@ __global__ __launch_bounds__(256) void k_route(RouteArgs a) {
     bad |= l[j] != l[j] || (!a.sigmoid && l[j] == INFINITY);
     m = fmaxf(m, l[j]);
   }
-  float bmax = 0.0f;
-  if (a.bias) {
+  float bmax = 0.0f, b[NE];                           // (past the row's end: any of its values)
 #pragma unroll
-    for (int j = 0; j < NE; ++j)
-      if (e0 + j < a.E) {
-        const float b = a.bias[e0 + j];
-        bad |= b != b;
-        bmax = fmaxf(bmax, fabsf(b) < INFINITY ? fabsf(b) : 0.0f);
-      }
+  for (int j = 0; j < NE; ++j) b[j] = 0.0f;
+  if (a.bias) {
+    if (a.vec) {
+      __builtin_memcpy(b, a.bias + e0, sizeof(b));
+    } else {
+#pragma unroll
+      for (int j = 0; j < NE; ++j) b[j] = a.bias[e0 + j < a.E ? e0 + j : 0];
+    }
+#pragma unroll
+    for (int j = 0; j < NE; ++j) {
+      bad |= b[j] != b[j];
+      bmax = fmaxf(bmax, fabsf(b[j]) < INFINITY ? fabsf(b[j]) : 0.0f);
+    }
   }
   bad = row_ballot<L>(bad) != 0;
   m = row_reduce<L>(m, [](float x, float y) { return fmaxf(x, y); });
@@ -167,8 +173,7 @@ __global__ __launch_bounds__(256) void k_route(RouteArgs a) {
       if (!wide) tol = 2 * ((a.sigmoid ? 5e-7f : 1e-6f) * top + 6e-8f * (top + (F)bmax)) * a.group_top;
 #pragma unroll
       for (int j = 0; j < NE; ++j) {
-        if (a.bias && e0 + j < a.E) key[j] += (F)a.bias[e0 + j];
-        if (l[j] == ninf) key[j] = lowest;
+        key[j] = l[j] == ninf ? lowest : key[j] + (F)b[j];
       }
     }
     bool sure = true;
