@@ -10,7 +10,7 @@ namespace gevo {
 constexpr int kRouteMaxE = 2048;      // experts a row is routed over
 constexpr int kRouteMaxK = 64;        // of them chosen for a row
 constexpr int kRouteMaxGroups = 64;
-constexpr int kPlanChunk = 2048;      // slots a workgroup of the plan kernels sorts
+constexpr int kPlanChunk = 1024;      // slots a workgroup of the plan kernels sorts
 
 struct RouteArgs {
   const void* logits; int64_t stride;  // [T] rows, elements apart

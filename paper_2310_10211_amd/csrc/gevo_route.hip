@@ -471,17 +471,24 @@ __global__ __launch_bounds__(1024) void k_plan_scan(uint32_t* counts, uint32_t* 
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, e = blockIdx.x * 64 + lane;
   const int per = (chunks + 15) / 16, c0 = wave * per, c1 = min(chunks, c0 + per);
   uint32_t sum = 0;
-  if (e < E)
+  if (e < E) {
+#pragma unroll 8
     for (int c = c0; c < c1; ++c) sum += counts[(size_t)c * E + e];
+  }
   part[wave][lane] = sum;
   __syncthreads();
   uint32_t at = 0;
   for (int w = 0; w < wave; ++w) at += part[w][lane];
   if (e >= E) return;
-  for (int c = c0; c < c1; ++c) {
-    const uint32_t n = counts[(size_t)c * E + e];
-    counts[(size_t)c * E + e] = at;
-    at += n;
+  for (int c = c0; c < c1; c += 8) {                 // eight loads at once, then their stores
+    uint32_t n[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) n[i] = c + i < c1 ? counts[(size_t)(c + i) * E + e] : 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      if (c + i < c1) counts[(size_t)(c + i) * E + e] = at;
+      at += n[i];
+    }
   }
   if (wave == 15) total[e] = at;
 }
