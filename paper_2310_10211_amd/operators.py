@@ -108,10 +108,22 @@ def _ptr(t):
     return None if t is None else t.data_ptr()
 
 
+def _u32_ok(name, value):
+    """value, which the library takes in 32 bits (ctypes would drop the others)."""
+    if not 0 <= value < 1 << 32:
+        raise GevoError(f"{name}: {value} does not fit 32 bits")
+    return value
+
+
 # The configurations of calls, by their values: a program repeats a few, and the
 # library reads them during the call alone.
 def _config(cls):
-    return functools.lru_cache(maxsize=1024)(lambda *values: ctypes.byref(cls(GEVO_ABI_VERSION, *values)))
+    def make(*values):
+        for (name, kind), value in zip(cls._fields_[1:], values):
+            if kind is _u32:
+                _u32_ok(name, value)
+        return ctypes.byref(cls(GEVO_ABI_VERSION, *values))
+    return functools.lru_cache(maxsize=1024)(make)
 
 
 _route_cfg, _expert_cfg = _config(RouteConfig), _config(ExpertConfig)
@@ -121,6 +133,7 @@ _combine_cfg, _mx4_cfg = _config(CombineConfig), _config(Mx4Config)
 @functools.lru_cache(maxsize=1024)
 def _plan_bytes(slots, n_experts):
     nbytes = ctypes.c_size_t()
+    _u32_ok("n_experts", n_experts)
     _check(lib().gevo_route_plan_bytes(slots, n_experts, ctypes.byref(nbytes)), "gevo_route_plan_bytes")
     return nbytes.value
 
@@ -326,7 +339,7 @@ class Mx4:
     __slots__ = ("codes", "scales", "k")
 
     def __init__(self, codes, scales, k):
-        if not (k >= 1 and isinstance(codes, torch.Tensor) and codes.is_cuda and codes.dim() >= 2):
+        if not (1 <= k < 1 << 32 and isinstance(codes, torch.Tensor) and codes.is_cuda and codes.dim() >= 2):
             raise GevoError("codes: a tensor [..., rows, Kp / 2] on the GPU")
         kp = (k + 127) // 128 * 128
         if codes.shape[-1] != kp // 2:
@@ -356,7 +369,7 @@ def mx4_quantize(x) -> Mx4:
         raise GevoError("x: a tensor [..., rows, K] on the GPU")
     if x.dtype not in DTYPES:
         raise GevoError(f"x: float32 or bfloat16, not {x.dtype}")
-    k = x.shape[-1]
+    k = _u32_ok("K", x.shape[-1])
     if x.dim() > 2 or (k > 1 and x.stride(-1) != 1) or (x.shape[0] > 1 and x.stride(0) < k):
         x = x.contiguous()
     kp = (k + 127) // 128 * 128

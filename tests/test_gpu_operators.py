@@ -587,3 +587,13 @@ def test_refused_tensors():
             lambda: g.Mx4(q.codes, q.scales, 200), lambda: g.Mx4(q.codes, q.scales[:2], 8)):
         with pytest.raises(g.GevoError):
             call()
+
+
+def test_refused_sizes():
+    x, ids = torch.zeros(4, 8, device="cuda"), torch.zeros(4, 2, dtype=torch.int32, device="cuda")
+    big = 1 << 32
+    for call in (lambda: g.route(x, big + 1), lambda: g.route(x, 1, groups=big + 1),
+                 lambda: g.route_plan(ids, big + 3),
+                 lambda: g.mx4_quantize(torch.empty(1, 1, device="cuda").expand(0, big + 128))):
+        with pytest.raises(g.GevoError):
+            call()

@@ -162,6 +162,20 @@ def test_python_refuses_host_tensors():
             call()
 
 
+def test_sizes_past_32_bits_are_refused():
+    from paper_2310_10211_amd import operators as o
+    _lib()
+    big = (1 << 32) + 1                              # 1 in its low 32 bits
+    for call in (lambda: o._route_cfg(8, big, 4, 0, 0, 8, 1, 1, 1, 1, 1.0),
+                 lambda: o._route_cfg(8, 2, 4, 0, 0, 8, big, 1, 1, 1, 1.0),
+                 lambda: o._expert_cfg(0, 0, 3, 2, big, 8, 4, 8, 40, 8, big, 0, 0),
+                 lambda: o._combine_cfg(0, 0, 2, big, 4, big, big), lambda: o._mx4_cfg(0, 3, 5, big, 4, 0, 1, 0, 0),
+                 lambda: o._plan_bytes(8, big), lambda: o._route_cfg(8, -1, 4, 0, 0, 8, 1, 1, 1, 1, 1.0)):
+        with pytest.raises(g.GevoError):
+            call()
+    assert o._route_cfg(8, 2, 4, 0, 0, 8, 1, 1, 1, 1, 1.0) is not None
+
+
 # ------------------------------------------------------------- the oracle itself
 def test_oracle_route_closed_forms():
     l = [math.log(4), math.log(1), math.log(3), -math.inf]
