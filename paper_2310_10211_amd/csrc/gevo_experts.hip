@@ -3,15 +3,16 @@
 // W_e^T, with W_e [N][K], and the two products of its gradient.
 //
 // k_expert_tile computes one tile of the output.  Operands of every type pass
-// through LDS alike, as rows of 64 bytes of contraction a step (16 fp32, 32
-// bf16, 128 4-bit values): 16-byte chunks, one a lane and matrix instruction.
+// through LDS alike, as rows of 128 or 64 bytes of contraction a step (32 or 16
+// fp32, 64 or 32 bf16, 256 or 128 4-bit values): 16-byte chunks, one a lane and
+// matrix instruction.
 // The order of the contraction inside a chunk is free as long as both operands
 // share it, so
 //   bf16   a chunk is one operand of a 32x32x16 instruction,
 //   fp32   its four values feed four 32x32x2 instructions,
 //   4 bit  it is one block of 32 values, whose scale is one byte of the lane's
 //          scale operand in a 32x32x64 instruction.
-// Three buffers hold a step in use and two under way.
+// Two buffers hold a step in use and one under way.
 #include "gevo_internal.h"
 #include "gevo_device.h"
 #include "gevo_ops.h"
@@ -32,8 +33,8 @@ typedef float f32x4_t __attribute__((ext_vector_type(4)));
 //          and 96 from LDS to the waves
 //   Mid    128 x 128
 //   Small  64 x 64: products of few tiles, spread over more of the chip
-// Two buffers hold a step in use and one under way.  Steps of 128 bytes read
-// whole cache lines.
+// Steps of 128 bytes read whole cache lines; Mid takes 64, whose buffers let
+// three workgroups share a CU.
 template <int RM_, int RN_, int MI_, int NI_, int WGS_, int STEP_>
 struct Shape {
   static constexpr int RM = RM_, RN = RN_, MI = MI_, NI = NI_, WGS = WGS_;
