@@ -32,7 +32,7 @@ __device__ __forceinline__ float exp_split(float x) {
 // A value rotated by N lanes within each 16.
 template <int N>
 __device__ __forceinline__ int rotated(int v) {
-  return __builtin_amdgcn_update_dpp(v, v, 0x120 + N, 0xf, 0xf, false);
+  return __builtin_amdgcn_update_dpp(0, v, 0x120 + N, 0xf, 0xf, true);
 }
 
 // Reductions over the L lanes (16 or 64, aligned) that share a row; f is
@@ -67,14 +67,27 @@ __device__ __forceinline__ uint64_t row_ballot(bool p) {
 
 }  // namespace
 
+// A binary32 as an integer that orders like it (no NaN; -0 below 0), and back;
+// binary64 keys stay what they are.
+__device__ __forceinline__ int ordered(float f) {
+  const int i = __builtin_bit_cast(int, f);
+  return i ^ ((i >> 31) & 0x7fffffff);
+}
+__device__ __forceinline__ double ordered(double f) { return f; }
+__device__ __forceinline__ float unordered(int i) { return __builtin_bit_cast(float, i ^ ((i >> 31) & 0x7fffffff)); }
+__device__ __forceinline__ double unordered(double f) { return f; }
+
 // Row t: scores s = softmax(l) or sigmoid(l), keys l or s + bias, the best
 // groups of keys, then the k largest keys among them (descending, ties to the
 // lowest index), weights scale s (renormalised over the choice).
 //
 // L lanes share a row, each holding NE consecutive logits.  A choice is the
-// row's largest local maximum and the lowest index that holds it; taking it out
-// redoes its lane's local maximum.  Bound by these instructions: a row of 256
-// logits needs about 90 for each choice of four rows.
+// row's largest local maximum and the lowest index that holds it, taken out by
+// the lane that has it.  Keys in 32 bits are compared as integers that order
+// like them, whose maximum of three is one instruction.  Bound by these
+// instructions (65,536 rows of 256, 8 groups, 8 chosen: 60 us, of which their
+// bytes take 13; 68 with keys compared as floats; finding the k-th key by
+// bisection took as long, a row in a whole wave 135).
 //
 // Two keys nearer than the rounding of 32-bit scores would be ordered by that
 // rounding: a row with such a pair among the keys (or groups) that decide its
@@ -109,11 +122,11 @@ __global__ __launch_bounds__(256) void k_route(RouteArgs a) {
   bool bad = false;                                  // NaN, or +inf under softmax: no scores
   float m = ninf;
 #pragma unroll
-  for (int j = 0; j < NE; ++j) {
-    bad |= l[j] != l[j] || (!a.sigmoid && l[j] == INFINITY);
-    m = fmaxf(m, l[j]);
+  for (int j = 0; j < NE; j += 2) {
+    bad |= __builtin_isunordered(l[j], l[j + 1]);
+    m = fmaxf(fmaxf(l[j], l[j + 1]), m);
   }
-  float bmax = 0.0f, b[NE];                           // (past the row's end: any of its values)
+  float bmax = 0.0f, b[NE];                          // (past the row's end: any of its values)
 #pragma unroll
   for (int j = 0; j < NE; ++j) b[j] = 0.0f;
   if (a.bias) {
@@ -124,46 +137,56 @@ __global__ __launch_bounds__(256) void k_route(RouteArgs a) {
       for (int j = 0; j < NE; ++j) b[j] = a.bias[e0 + j < a.E ? e0 + j : 0];
     }
 #pragma unroll
-    for (int j = 0; j < NE; ++j) {
-      bad |= b[j] != b[j];
-      bmax = fmaxf(bmax, fabsf(b[j]) < INFINITY ? fabsf(b[j]) : 0.0f);
+    for (int j = 0; j < NE; j += 2) {
+      bad |= __builtin_isunordered(b[j], b[j + 1]);
+      bmax = fmaxf(fmaxf(fabsf(b[j]), fabsf(b[j + 1])), bmax);
+    }
+    if (__any(bmax == INFINITY)) {                   // the largest finite one
+      bmax = 0.0f;
+#pragma unroll
+      for (int j = 0; j < NE; ++j) bmax = fmaxf(bmax, fabsf(b[j]) < INFINITY ? fabsf(b[j]) : 0.0f);
     }
   }
-  bad = row_ballot<L>(bad) != 0;
   m = row_reduce<L>(m, [](float x, float y) { return fmaxf(x, y); });
   bmax = row_reduce<L>(bmax, [](float x, float y) { return fmaxf(x, y); });
+  bad = row_ballot<L>(bad || (!a.sigmoid && m == INFINITY)) != 0;
 
   // the choice with keys of type F; returns whether its order is beyond doubt
   int chosen = -1;                                   // lane j of the row: the j-th choice
+  __shared__ int picked[kRows][L];                   // of a row: its choices
   const int gs = a.E / a.groups;
   auto choose = [&](auto zero) -> bool {
     typedef decltype(zero) F;
+    typedef decltype(ordered(zero)) K;
     constexpr bool wide = sizeof(F) == 8;
-    const F lowest = (F)ninf;
-    F key[NE];
-    F tol = 0, sum = 0;
+    const F flowest = (F)ninf;
+    const K lowest = ordered(flowest);
+    auto more = [](K x, K y) { return x > y ? x : y; };
+    auto less = [](K x, K y) { return x < y ? x : y; };
+    K key[NE];
+    F tol = 0;
     if (a.by_logit) {
 #pragma unroll
-      for (int j = 0; j < NE; ++j) key[j] = (F)l[j];
+      for (int j = 0; j < NE; ++j) key[j] = ordered((F)l[j] + (F)0);   // (-0 is 0)
     } else {
-      F top = 1;
+      F score[NE], sum = 0, top = 1;
       if (a.sigmoid) {
 #pragma unroll
         for (int j = 0; j < NE; ++j) {
-          if constexpr (wide) key[j] = 1.0 / (1.0 + exp(-(double)l[j]));
-          else key[j] = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(l[j] * -1.44269504f));
+          if constexpr (wide) score[j] = 1.0 / (1.0 + exp(-(double)l[j]));
+          else score[j] = __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(l[j] * -1.44269504f));
         }
       } else {
 #pragma unroll
         for (int j = 0; j < NE; ++j) {
-          if constexpr (wide) key[j] = l[j] == ninf ? 0.0 : exp((double)l[j] - (double)m);
-          else key[j] = l[j] == ninf ? 0.0f : __builtin_amdgcn_exp2f((l[j] - m) * 1.44269504f);
-          sum += key[j];
+          if constexpr (wide) score[j] = l[j] == ninf ? 0.0 : exp((double)l[j] - (double)m);
+          else score[j] = l[j] == ninf ? 0.0f : __builtin_amdgcn_exp2f((l[j] - m) * 1.44269504f);
+          sum += score[j];
         }
         sum = row_reduce<L>(sum, [](F x, F y) { return x + y; });
         top = (F)1 / sum;                            // the row's largest score
 #pragma unroll
-        for (int j = 0; j < NE; ++j) key[j] *= top;
+        for (int j = 0; j < NE; ++j) score[j] *= top;
       }
       // What two keys in 32 bits can be off by together.  exp2's argument is
       // rounded to |x| 2^-24 log2 e, which x s (1 - s) <= 0.23 and d e^-d <= 0.37
@@ -172,9 +195,7 @@ __global__ __launch_bounds__(256) void k_route(RouteArgs a) {
       // the bias half a step of itself; a group adds two keys.
       if (!wide) tol = 2 * ((a.sigmoid ? 5e-7f : 1e-6f) * top + 6e-8f * (top + (F)bmax)) * a.group_top;
 #pragma unroll
-      for (int j = 0; j < NE; ++j) {
-        key[j] = l[j] == ninf ? lowest : key[j] + (F)b[j];
-      }
+      for (int j = 0; j < NE; ++j) key[j] = ordered(l[j] == ninf ? flowest : score[j] + (F)b[j]);
     }
     bool sure = true;
     if (a.groups > 1) {
@@ -182,23 +203,22 @@ __global__ __launch_bounds__(256) void k_route(RouteArgs a) {
       // 1, 2, 4 .. whole lanes hold a group, else through LDS (lane g: group g)
       const int per = gs / NE;                       // lanes of a group
       const bool inreg = gs % NE == 0 && (per & (per - 1)) == 0;
-      F v1 = lowest, v2 = lowest;                    // its largest keys
-      auto take = [&](F x) {
-        v2 = x > v1 ? v1 : (x > v2 ? x : v2);
-        v1 = x > v1 ? x : v1;
+      K v1 = lowest, v2 = lowest;                    // its largest keys
+      auto take = [&](K x) {
+        v2 = more(v2, less(v1, x));
+        v1 = more(v1, x);
       };
-      int mine = lane;                               // the group whose value the lane holds
+      const int shift = inreg ? __ffs(per) - 1 : 0;  // lane >> shift: the group whose value the lane holds
       if (inreg) {
 #pragma unroll
         for (int j = 0; j < NE; ++j) take(key[j]);
         for (int d = 1; d < per; d <<= 1) {
-          const F o1 = __shfl_xor(v1, d, L), o2 = __shfl_xor(v2, d, L);
+          const K o1 = __shfl_xor(v1, d, L), o2 = __shfl_xor(v2, d, L);
           take(o1);
           take(o2);
         }
-        mine = lane / per;
       } else {
-        F* ks = reinterpret_cast<F*>(smem) + (size_t)rw * (L * NE);
+        K* ks = reinterpret_cast<K*>(smem) + (size_t)rw * (L * NE);
 #pragma unroll
         for (int j = 0; j < NE; ++j) ks[e0 + j] = key[j];
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
@@ -206,20 +226,23 @@ __global__ __launch_bounds__(256) void k_route(RouteArgs a) {
           for (int i = 0; i < gs; ++i) take(ks[lane * gs + i]);
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
       }
-      F v = a.group_top == 2 && v2 > lowest ? v1 + v2 : v1;
-      if (mine >= a.groups) v = lowest;
+      const int mine = lane >> shift;
+      F v = a.group_top == 2 && v2 > lowest ? unordered(v1) + unordered(v2) : unordered(v1);
+      if (mine >= a.groups) v = flowest;
       uint64_t stay = 0;
-      F last = lowest;
+      F last = flowest;
       for (int i = 0; i <= a.top_groups && i < a.groups; ++i) {
         const F mx = row_reduce<L>(v, [](F x, F y) { return x > y ? x : y; });
         if (i == a.top_groups) {
-          if (!(last - mx > tol) && last > lowest) sure = false;
+          if (!(last - mx > tol) && last > flowest) sure = false;
           break;
         }
-        const int g = row_reduce<L>(v == mx && mine < a.groups ? mine : 64, [](int x, int y) { return x < y ? x : y; });
-        if (g < 64) stay |= 1ull << g;
+        // lanes and groups ascend together: the first lane has the lowest group
+        const uint64_t hold = row_ballot<L>(v == mx);
+        const int g = (__ffsll((unsigned long long)hold) - 1) >> shift;
+        if (hold) stay |= 1ull << (g & 63);
         last = mx;
-        if (mine == g) v = lowest;
+        if (mine == g) v = flowest;
       }
       if (inreg) {
         const bool in = (stay >> (mine & 63)) & 1;
@@ -234,30 +257,39 @@ __global__ __launch_bounds__(256) void k_route(RouteArgs a) {
         }
       }
     }
-    F lm = lowest;
+    auto largest = [&]() {
+      K v = lowest;
 #pragma unroll
-    for (int j = 0; j < NE; ++j) lm = key[j] > lm ? key[j] : lm;
-    chosen = -1;
-    F last = lowest;
+      for (int j = 0; j < NE; j += 2) v = more(more(key[j], key[j + 1]), v);
+      return v;
+    };
+    K lm = largest();
+    picked[rw][lane] = -1;
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    K last = lowest;
     const int tries = wide || a.by_logit ? a.k : a.k + 1;   // the first key left out is looked at, too
     for (int i = 0; i < tries; ++i) {
-      const F mx = row_reduce<L>(lm, [](F x, F y) { return x > y ? x : y; });
-      if (i > 0 && !wide && !a.by_logit && last > lowest && !(last - mx > tol)) sure = false;
+      const K mx = row_reduce<L>(lm, more);
+      if (!wide && !a.by_logit && i > 0 && last > lowest && !(unordered(last) - unordered(mx) > tol)) sure = false;
       if (i == a.k) break;
       last = mx;
-      int at = NE;                                   // the first of the lane's that is as large
-#pragma unroll
-      for (int j = NE - 1; j >= 0; --j) at = key[j] == mx ? j : at;
-      const int none = 1 << 30;
-      const int e = row_reduce<L>(at < NE && mx > lowest ? e0 + at : none, [](int x, int y) { return x < y ? x : y; });
-      if (lane == i) chosen = e < none ? e : -1;
-      lm = lowest;
+      const uint64_t hold = row_ballot<L>(lm == mx && mx > lowest);
+      const bool owner = lane == __ffsll((unsigned long long)hold) - 1;
+      bool left = owner;                             // the first of its keys that is as large goes
+      int at = 0;
 #pragma unroll
       for (int j = 0; j < NE; ++j) {
-        key[j] = e0 + j == e ? lowest : key[j];
-        lm = key[j] > lm ? key[j] : lm;
+        const bool hit = left && key[j] == mx;
+        at = hit ? j : at;
+        key[j] = hit ? lowest : key[j];
+        left = left && !hit;
       }
+      lm = largest();
+      if (owner) picked[rw][i] = e0 + at;
     }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    chosen = picked[rw][lane];
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     return sure;
   };
   const bool none = bad || m == ninf;
