@@ -149,18 +149,35 @@ __device__ __forceinline__ void segment(const ExpertArgs& a, int e, int64_t& s0,
 }
 
 // row of x that row i of segment e (its first sorted row s0) reads; -1: none
-__device__ __forceinline__ int64_t placed_row(const int32_t* order, int k, int64_t rows, int64_t r) {
-  if (order) r = (uint32_t)order[r] / (uint32_t)k;
+__device__ __forceinline__ int64_t placed_row(const ExpertArgs& a, const int32_t* order, int64_t rows, int64_t r) {
+  if (order) {
+    const uint32_t slot = (uint32_t)order[r];
+    r = a.k > 1 ? __umulhi(slot, a.k_mul) >> a.k_shift : slot;   // slot / k
+  }
   return r < rows ? r : -1;
 }
 __device__ __forceinline__ int64_t source_row(const ExpertArgs& a, int64_t s0, int64_t i) {
-  return a.offsets ? placed_row(a.order, a.k, a.xrows, s0 + i) : i;
+  return a.offsets ? placed_row(a, a.order, a.xrows, s0 + i) : i;
+}
+
+// Tile idx of rt x nt: eight row tiles at a time, for all column tiles, the row
+// tiles fastest.  An XCD's 32 CUs then work on about 8 x 4 tiles, whose 12
+// operand tiles are the fewest for 32 (all row tiles first: 33 of them).  A CU
+// has only so many lines under way, so what it takes in a clock goes by the time
+// a line takes, which a miss in L2 makes long: one 8192 x 8192 matrix on 8,192
+// rows in bf16, with its join, 987 us; all row tiles first, 1,107.
+struct Place {
+  uint32_t row, col;
+};
+__device__ __forceinline__ Place grouped(uint32_t idx, uint32_t rt, uint32_t nt, uint32_t most = 8) {
+  most = min(most, rt);
+  const uint32_t g = idx / (most * nt), left = idx - g * (most * nt), here = min(most, rt - g * most);
+  return {g * most + left % here, left / here};
 }
 
 // Workgroup -> tile of a list, of which XCD j (workgroups with index j mod 8)
 // gets the j-th eighth, so that the tiles that read the same operands run near
-// each other under one L2.  Routed rows: expert by expert, each expert's tiles
-// column tile by column tile with the row tiles fastest.  Every wave sums the
+// each other under one L2.  Routed rows: expert by expert.  Every wave sums the
 // experts' tile counts, 64 at a time.
 struct Tile {
   int e, nt;
@@ -198,12 +215,11 @@ __device__ __forceinline__ bool find_tile(const ExpertArgs& a, int ntiles, Tile&
     // pass by (64 variants of 784-512 over 10,000 rows in 4 bits 327 us;
     // an eighth of the matrices to each XCD, as where rows differ, 343).
     const uint32_t rts = (uint32_t)((a.M + kXR - 1) / kXR), all = (uint32_t)a.E * (uint32_t)ntiles;
-    const uint32_t group = a.x_e == 0 ? (rts + 7) / 8 : rts, g = idx / (group * all);
-    idx -= g * group * all;
-    const uint32_t here = min(group, rts - g * group), c = idx / here;
-    o.e = __builtin_amdgcn_readfirstlane((int)(c / (uint32_t)ntiles));
-    o.nt = __builtin_amdgcn_readfirstlane((int)(c % (uint32_t)ntiles));
-    o.m0 = (int64_t)(g * group + __builtin_amdgcn_readfirstlane((int)(idx % here))) * kXR;
+    const Place in = grouped(idx, rts, all, a.x_e == 0 ? max(1u, min(8u, (rts + 7) / 8)) : 8);
+    const uint32_t c = (uint32_t)__builtin_amdgcn_readfirstlane((int)in.col);
+    o.e = (int)(c / (uint32_t)ntiles);
+    o.nt = (int)(c % (uint32_t)ntiles);
+    o.m0 = (int64_t)__builtin_amdgcn_readfirstlane((int)in.row) * kXR;
     segment(a, o.e, o.s0, o.cnt);
     return true;
   } else {
@@ -212,6 +228,7 @@ __device__ __forceinline__ bool find_tile(const ExpertArgs& a, int ntiles, Tile&
       const uint32_t sum = a.E > 64 ? look(b) : total;   // (up to 64: still in the lanes)
       if (idx < sum) {
         const uint64_t in = __ballot(idx >= before && idx < before + mine);
+        if (in == 0) return false;                   // (offsets of no plan, whose counts pass 32 bits)
         const int l = __ffsll((unsigned long long)in) - 1;
         o.e = b + l;
         idx -= (uint32_t)__builtin_amdgcn_readlane((int)before, __builtin_amdgcn_readfirstlane(l));
@@ -224,8 +241,9 @@ __device__ __forceinline__ bool find_tile(const ExpertArgs& a, int ntiles, Tile&
   idx = (uint32_t)__builtin_amdgcn_readfirstlane((int)idx);
   segment(a, o.e, o.s0, o.cnt);
   const uint32_t rt = (uint32_t)((o.cnt + kXR - 1) / kXR);
-  o.nt = (int)(idx / rt);
-  o.m0 = (int64_t)(idx % rt) * kXR;
+  const Place in = grouped(idx, rt, (uint32_t)ntiles);
+  o.nt = __builtin_amdgcn_readfirstlane((int)in.col);
+  o.m0 = (int64_t)__builtin_amdgcn_readfirstlane((int)in.row) * kXR;
   return true;
 }
 
@@ -313,9 +331,9 @@ __global__ __launch_bounds__(SH::kThreads, SH::WGS* SH::kThreads / 256) void k_e
     const uint32_t at = blockIdx.x >> 3, idx = (blockIdx.x & 7) * each + at;
     if (at >= each || idx >= total) return;
     tl.e = (int)(idx / (uint32_t)(nr * nc));
-    const int in = (int)(idx % (uint32_t)(nr * nc));
-    tl.nt = in / nr;
-    tl.m0 = (int64_t)(in % nr) * kXR;
+    const Place in = grouped(idx % (uint32_t)(nr * nc), (uint32_t)nr, (uint32_t)nc);
+    tl.nt = (int)in.col;
+    tl.m0 = (int64_t)in.row * kXR;
     segment(a, tl.e, tl.s0, tl.cnt);
   } else {
     if (!find_tile<kXR>(a, (a.N + kWR - 1) / kWR, tl)) return;
@@ -334,6 +352,8 @@ __global__ __launch_bounds__(SH::kThreads, SH::WGS* SH::kThreads / 256) void k_e
   const char* wp[NWL];
   uint32_t have = 0;                                 // bit j: load j of x has a row, bit 16 + j: of w
   const char* zero = (const char*)&g_zero_chunk;
+  bool there = true;                                 // the lane's rows that have a place have a source
+  bool have_s = false;
   const char* sp = nullptr;                          // 4-bit operands: a wave loads 64 rows' scales
   constexpr int kSx = kXR / 64, kSn = (kXR + kWR) / 64;
   const int sj = wu % kSn;
@@ -345,8 +365,12 @@ __global__ __launch_bounds__(SH::kThreads, SH::WGS* SH::kThreads / 256) void k_e
       for (int j = 0; j < NXL; ++j) {
         const int64_t i = tl.m0 + kLR * (NXL * wave + j) + crow;
         int64_t r = i < tl.cnt ? source_row(a, tl.s0, i) : -1;
-        if (r >= 0) have |= 1u << j;
-        else r = 0;
+        if (r >= 0) {
+          have |= 1u << j;
+        } else {
+          there &= i >= tl.cnt;
+          r = 0;
+        }
         xp[j] = (const char*)a.x + (a.offsets ? 0 : tl.e * a.x_e) + r * a.x_stride + cb[j & 1];
       }
     }
@@ -359,14 +383,16 @@ __global__ __launch_bounds__(SH::kThreads, SH::WGS* SH::kThreads / 256) void k_e
       }
     }
     if constexpr (mx) {
-      sp = nullptr;
       if (sj < kSx) {
         const int64_t i = tl.m0 + 64 * sj + lane;
         const int64_t r = i < tl.cnt ? source_row(a, tl.s0, i) : -1;
-        if (r >= 0) sp = (const char*)a.xs + (a.offsets ? 0 : tl.e * a.xs_e) + r * a.xs_stride;
+        have_s = r >= 0;
+        there &= have_s || i >= tl.cnt;
+        sp = (const char*)a.xs + (a.offsets ? 0 : tl.e * a.xs_e) + (have_s ? r : 0) * a.xs_stride;
       } else {
         const int n = n0 + 64 * (sj - kSx) + lane;
-        if (n < a.N) sp = (const char*)a.ws + tl.e * a.ws_e + n * a.ws_n;
+        have_s = n < a.N;
+        sp = (const char*)a.ws + tl.e * a.ws_e + (have_s ? n : 0) * a.ws_n;
       }
     }
   }
@@ -381,13 +407,15 @@ __global__ __launch_bounds__(SH::kThreads, SH::WGS* SH::kThreads / 256) void k_e
     int row0, per;                                   // the lane's row in the wave's first load; rows a load
     int cb[2];                                       // its column's byte in even and odd loads, -1: none
     int drop[2], valid[2];                           // elements of the chunk before that column; that exist
+    const char* first[2];                            // that column's address in the lane's first row (gathered: row 0)
+    int64_t load, step;                              // bytes between the rows of two loads, of two steps
   } nx{}, nw{};
   auto natural_block = [](int tile_bytes, int row) {  // what the row's 16-byte chunks are xored with
     if (sizeof(S) == 4) return ((row >> 2) & 1) << 3;
     return (tile_bytes == 128 ? (row >> 1) & 1 : row & 3) << 2;
   };
   auto natural_setup = [&](Natural& d, const char* base, int64_t stride, int tile_rows, int loads, int col0, int width,
-                           bool guarded) {
+                           bool guarded, bool placed) {
     const int tb = tile_rows * (int)sizeof(S);       // bytes of a tile's row
     d.base = base;
     d.stride = stride;
@@ -401,13 +429,16 @@ __global__ __launch_bounds__(SH::kThreads, SH::WGS* SH::kThreads / 256) void k_e
       d.drop[v] = over > 0 && over < 16 ? over / (int)sizeof(S) : 0;
       d.valid[v] = over < 16 ? V - (over > 0 ? over / (int)sizeof(S) : 0) : 0;
       d.cb[v] = over >= 16 ? -1 : guarded ? c : c - (over > 0 ? over : 0);
+      d.first[v] = base + (placed ? 0 : d.row0 * stride) + (d.cb[v] < 0 ? 0 : d.cb[v]);
     }
+    d.load = d.per * stride;
+    d.step = kPer * stride;
   };
   if constexpr (by_index(XL))                        // dw: columns of dy
-    natural_setup(nx, (const char*)a.w + tl.s0 * a.w_n, a.w_n, kXR, NXL, (int)tl.m0, a.N, XL != kNatural);
+    natural_setup(nx, (const char*)a.w + tl.s0 * a.w_n, a.w_n, kXR, NXL, (int)tl.m0, a.N, XL != kNatural, false);
   if constexpr (by_index(WL)) {
-    if constexpr (PASS == kDw) natural_setup(nw, (const char*)a.x, a.x_stride, kWR, NWL, n0, a.K, WL != kNatural);
-    else natural_setup(nw, (const char*)a.w + tl.e * a.w_e, a.w_n, kWR, NWL, n0, a.N, WL != kNatural);
+    if constexpr (PASS == kDw) natural_setup(nw, (const char*)a.x, a.x_stride, kWR, NWL, n0, a.K, WL != kNatural, true);
+    else natural_setup(nw, (const char*)a.w + tl.e * a.w_e, a.w_n, kWR, NWL, n0, a.N, WL != kNatural, false);
   }
   int32_t gathered[PASS == kDw ? NWL : 1];   // rows of x that the next step's loads read
   auto gather = [&](int st) {
@@ -451,10 +482,53 @@ __global__ __launch_bounds__(SH::kThreads, SH::WGS* SH::kThreads / 256) void k_e
     }
     n -= kWi;
     if constexpr (mx)
-      dma4_at(sp && st * kC + n * 4 < bytes / 16 ? sp + st * kC + n * 4 : zero,
+      dma4_at(have_s && st * kC + n * 4 < bytes / 16 ? sp + st * kC + n * 4 : zero,
               buf + kXBytes + kWBytes + (uint32_t)n * (kXR + kWR) * 4u + (uint32_t)sj * 256u);
   };
+  // The same where step st lies inside every operand and no row is out of place:
+  // an address a load, without a look at what exists (which took 30 instructions
+  // a load: 8,192 rows through 4 of 64 experts of 2048 x 2048 434 us, so 419).
+  // Rows and columns outside the operands read the first ones, and their products
+  // are not written.
+  const bool plain = kAllDma && __all(there);
+  auto inside = [&](int st) {
+    bool in = plain && st < nst;
+    if constexpr (by_index(XL) || by_index(WL)) in = in && (int64_t)(st + 1) * kPer <= clen;
+    if constexpr (PASS != kDw) in = in && (st + 1) * kStep <= bytes;
+    if constexpr (PASS == kDw) {
+      int32_t low = gathered[0];
+#pragma unroll
+      for (int n = 1; n < NWL; ++n) low = min(low, gathered[n]);
+      in = in && __all(low >= 0);
+    }
+    return in;
+  };
+  auto issue_inside = [&](int st, int b, int n) {
+    const uint32_t buf = (uint32_t)__builtin_amdgcn_readfirstlane((int)(lds0 + (uint32_t)b * kBuf));
+    if (n < kXi) {
+      const uint32_t to = buf + (uint32_t)(NXL * wu + n) * 1024u;
+      if constexpr (XL == kDma) dma16_at(xp[n] + (int64_t)st * kStep, to);
+      else dma16_at(nx.first[n & 1] + (st * nx.step + n * nx.load), to);
+      return;
+    }
+    n -= kXi;
+    if (n < kWi) {
+      const uint32_t to = buf + kXBytes + (uint32_t)(NWL * wu + n) * 1024u;
+      if constexpr (WL == kDma) dma16_at(wp[n] + (int64_t)st * kStep, to);
+      else if constexpr (PASS == kDw) dma16_at(nw.first[n & 1] + (uint32_t)gathered[n] * nw.stride, to);
+      else dma16_at(nw.first[n & 1] + (st * nw.step + n * nw.load), to);
+      return;
+    }
+    n -= kWi;
+    if constexpr (mx)
+      dma4_at(sp + (int64_t)st * kC + n * 4, buf + kXBytes + kWBytes + (uint32_t)n * (kXR + kWR) * 4u + (uint32_t)sj * 256u);
+  };
   auto issue = [&](int st, int b) {
+    if (inside(st)) {
+#pragma unroll
+      for (int n = 0; n < kIssued; ++n) issue_inside(st, b, n);
+      return;
+    }
 #pragma unroll
     for (int n = 0; n < kIssued; ++n) issue_one(st, b, n);
   };
@@ -651,8 +725,7 @@ __global__ __launch_bounds__(SH::kThreads, SH::WGS* SH::kThreads / 256) void k_e
   constexpr int kTs = kRowB / (32 * (int)sizeof(O));                                         // column tiles a round
   constexpr int kCh = kRowB / 16, kEl = 16 / (int)sizeof(O);
   static_assert(SH::kWaves * 32 * kRowB <= kXBytes + kWBytes, "the output's staging fits a buffer");
-  float* bs = reinterpret_cast<float*>(smem + 2 * kBuf);       // the tile's biases
-  const bool biased = PASS == kForward && a.bias;
+  float* bs = reinterpret_cast<float*>(smem + 2 * kBuf);       // the tile's biases, which the sums start from
   const bool whole = ((cols | (int)(a.out_stride % kEl)) & (kEl - 1)) == 0 && (uintptr_t)a.out % 16 == 0;
 
   const bool sums = PASS == kDw && a.db && tl.nt == 0;
@@ -660,7 +733,7 @@ __global__ __launch_bounds__(SH::kThreads, SH::WGS* SH::kThreads / 256) void k_e
 #pragma unroll
   for (int i = 0; i < (kSums ? MI : 1); ++i) col_sum[i] = 0.0f;
   float bias = 0.0f;
-  if (biased && tid < kWR && n0 + tid < a.N) bias = a.bias[(int64_t)tl.e * a.N + n0 + tid];
+  if (PASS == kForward && a.bias && tid < kWR && n0 + tid < a.N) bias = a.bias[(int64_t)tl.e * a.N + n0 + tid];
 #pragma unroll
   for (int i = 0; i < MI; ++i)
 #pragma unroll
@@ -681,8 +754,25 @@ __global__ __launch_bounds__(SH::kThreads, SH::WGS* SH::kThreads / 256) void k_e
     if (nst > 1) wait_vm<kIssued>();
     else wait_vm<0>();
     settle(0, 0);
+    if (PASS == kForward && tid < kWR) bs[tid] = bias;
     __syncthreads();
     if (has_rows) {
+      if constexpr (PASS == kForward) {
+#pragma unroll
+        for (int t = 0; t < NI; ++t)
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            const float4 c = *reinterpret_cast<const float4*>(bs + wn * 32 * NI + 32 * t + 8 * q + 4 * lh);
+            acc[0][t][4 * q] = c.x;
+            acc[0][t][4 * q + 1] = c.y;
+            acc[0][t][4 * q + 2] = c.z;
+            acc[0][t][4 * q + 3] = c.w;
+          }
+#pragma unroll
+        for (int i = 1; i < MI; ++i)
+#pragma unroll
+          for (int t = 0; t < NI; ++t) acc[i][t] = acc[0][t];
+      }
       read_x(0, 0);
 #pragma unroll
       for (int t = 0; t < NI; ++t) read_w(0, 0, t);
@@ -724,12 +814,16 @@ __global__ __launch_bounds__(SH::kThreads, SH::WGS* SH::kThreads / 256) void k_e
       }
       if (has_rows && (!mx || filled == kQ)) {
         if (adds) add_columns(1);
+        const bool in = inside(st + 2);
         if (more) read_x(b ^ 1, 0);
 #pragma unroll
         for (int t = 0; t < NI; ++t) {
           if (more) read_w(b ^ 1, 0, t);
           mul(std::integral_constant<int, 1>{}, t);
-          if (ahead) {
+          if (in) {
+#pragma unroll
+            for (int n = t * kIssued / NI; n < (t + 1) * kIssued / NI; ++n) issue_inside(st + 2, b, n);
+          } else if (ahead) {
 #pragma unroll
             for (int n = t * kIssued / NI; n < (t + 1) * kIssued / NI; ++n) issue_one(st + 2, b, n);
           }
@@ -754,10 +848,13 @@ __global__ __launch_bounds__(SH::kThreads, SH::WGS* SH::kThreads / 256) void k_e
 
   // ---- output
   __syncthreads();                                 // every wave is past its reads of the buffers
-  if (biased && tid < kWR) bs[tid] = bias;
-  __syncthreads();
   if (has_rows) {
     char* stage = smem + wu * 32 * kRowB;
+    const float least = PASS == kForward && a.relu ? 0.0f : -INFINITY;
+    // the lane's row and column in the first of the band's rounds
+    const int64_t r0 = tl.m0 + wm * 32 * MI + lane / kCh;
+    const int c0 = n0 + wn * 32 * NI + lane % kCh * kEl;
+    O* const o0 = (O*)a.out + (PASS == kDw ? (int64_t)tl.e * a.N + r0 : tl.s0 + r0) * a.out_stride + c0;
 #pragma unroll
     for (int i = 0; i < MI; ++i)
 #pragma unroll
@@ -769,13 +866,9 @@ __global__ __launch_bounds__(SH::kThreads, SH::WGS* SH::kThreads / 256) void k_e
             float f[4];
 #pragma unroll
             for (int u = 0; u < 4; ++u) f[u] = acc[i][t][4 * q + u];
-            if (biased) {
-              const float4 c = *reinterpret_cast<const float4*>(bs + wn * 32 * NI + 32 * t + 8 * q + 4 * lh);
-              f[0] += c.x; f[1] += c.y; f[2] += c.z; f[3] += c.w;
-            }
-            if (PASS == kForward && a.relu) {
+            if constexpr (PASS == kForward) {
 #pragma unroll
-              for (int u = 0; u < 4; ++u) f[u] = f[u] < 0.0f ? 0.0f : f[u];   // (NaN stays)
+              for (int u = 0; u < 4; ++u) f[u] = f[u] < least ? least : f[u];   // (NaN stays)
             }
             char* row = stage + l32 * kRowB;
             if constexpr (OUT16) {                 // chunk 4 t + q, half lh
@@ -791,12 +884,12 @@ __global__ __launch_bounds__(SH::kThreads, SH::WGS* SH::kThreads / 256) void k_e
         for (int j = 0; j < kCh / 2; ++j) {        // 64 / kCh rows an instruction
           const int rr = j * (64 / kCh) + lane / kCh, ch = lane % kCh;
           uint4 u = *reinterpret_cast<const uint4*>(stage + rr * kRowB + 16 * (ch ^ (rr & (kCh - 1))));
-          const int64_t r = tl.m0 + wm * 32 * MI + 32 * i + rr;
-          const int c = n0 + wn * 32 * NI + 32 * t0 + ch * kEl;
+          const int64_t r = r0 + (32 * i + j * (64 / kCh));
+          const int c = c0 + 32 * t0;
           if (r >= rows || c >= cols) continue;
           if constexpr (PASS == kDx && !mx) {
             if (a.mask) {
-              const int64_t mr = placed_row(a.mask_order, a.k, a.mask_rows, tl.s0 + r);
+              const int64_t mr = placed_row(a, a.mask_order, a.mask_rows, tl.s0 + r);
               const char* mp = (const char*)a.mask + (mr < 0 ? 0 : mr) * a.mask_stride + (size_t)c * sizeof(S);
               const uint4 mu = load_chunk<S>(mp, cols - c, n0 + kWR > cols, cols >= V, (const char*)a.mask);
               S me[V];
@@ -810,8 +903,7 @@ __global__ __launch_bounds__(SH::kThreads, SH::WGS* SH::kThreads / 256) void k_e
               __builtin_memcpy(&u, oe, 16);
             }
           }
-          const int64_t orow = PASS == kDw ? (int64_t)tl.e * a.N + r : tl.s0 + r;
-          O* o = (O*)a.out + orow * a.out_stride + c;
+          O* o = o0 + ((32 * i + j * (64 / kCh)) * a.out_stride + 32 * t0);
           if (whole) {
             *reinterpret_cast<uint4*>(o) = u;
           } else {
@@ -947,6 +1039,17 @@ __global__ __launch_bounds__(256, 4) void k_expert_few(ExpertArgs a) {
 
 namespace {
 
+// Division of slots, below 2^31, by k > 1: with 2^s >= k the smallest, m =
+// floor(2^(31 + s) / k) + 1 exceeds 2^(31 + s) / k by at most 2^s / 2^(31 + s)
+// relative, so slot m / 2^(31 + s) exceeds slot / k by less than 1 / k.
+ExpertArgs with_divisor(ExpertArgs a) {
+  int s = 1;
+  while (((int64_t)1 << s) < a.k) ++s;
+  a.k_mul = a.k > 1 ? (uint32_t)((1ull << (31 + s)) / (uint32_t)a.k + 1) : 0;
+  a.k_shift = s - 1;
+  return a;
+}
+
 template <typename SH, ExpertType TY, Pass PASS, Load XL, Load WL, bool OUT16>
 hipError_t tile_go(const ExpertArgs& a, int64_t tiles, hipStream_t s) {
   constexpr size_t lds =
@@ -1044,7 +1147,8 @@ hipError_t dx_go(const ExpertArgs& a, hipStream_t s) {
 
 }  // namespace
 
-hipError_t launch_expert_forward(const ExpertArgs& a, ExpertType type, bool out_bf16, hipStream_t s) {
+hipError_t launch_expert_forward(const ExpertArgs& args, ExpertType type, bool out_bf16, hipStream_t s) {
+  const ExpertArgs a = with_divisor(args);
   switch (type) {
     case kTypeF32: return out_bf16 ? forward_out<kTypeF32, true>(a, s) : forward_out<kTypeF32, false>(a, s);
     case kTypeBf16: return out_bf16 ? forward_out<kTypeBf16, true>(a, s) : forward_out<kTypeBf16, false>(a, s);
@@ -1052,11 +1156,13 @@ hipError_t launch_expert_forward(const ExpertArgs& a, ExpertType type, bool out_
   }
 }
 
-hipError_t launch_expert_dx(const ExpertArgs& a, ExpertType type, hipStream_t s) {
+hipError_t launch_expert_dx(const ExpertArgs& args, ExpertType type, hipStream_t s) {
+  const ExpertArgs a = with_divisor(args);
   return type == kTypeF32 ? dx_go<kTypeF32>(a, s) : dx_go<kTypeBf16>(a, s);
 }
 
-hipError_t launch_expert_dw(const ExpertArgs& a, ExpertType type, hipStream_t s) {
+hipError_t launch_expert_dw(const ExpertArgs& args, ExpertType type, hipStream_t s) {
+  const ExpertArgs a = with_divisor(args);
   const int64_t e = type == kTypeF32 ? 4 : 2;
   const bool aligned = on_dwords(a.K * e, a.x, a.x_stride, 0) && on_dwords(a.N * e, a.w, a.w_n, 0);
   if (type == kTypeF32)

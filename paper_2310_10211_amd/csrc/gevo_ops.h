@@ -61,6 +61,7 @@ struct ExpertArgs {
   const int32_t* offsets;                  // [E + 1]
   const int32_t* order;                    // row of x of sorted row s: order[s] / k (null: s; dense: its place)
   int k; int64_t xrows;                    // rows of x (a place beyond them reads zeros)
+  uint32_t k_mul; int k_shift;             // set by the launcher: slot / k = slot k_mul / 2^(32 + k_shift)
   const void* x; int64_t x_stride, x_e;    // bytes between rows, and (dense) between segments
   const void* w; int64_t w_e, w_n;         // bytes between experts, between rows of a matrix
   const uint8_t* xs; int64_t xs_stride, xs_e;   // 4-bit operands: scales
