@@ -74,6 +74,24 @@ def _flat(t, name, dtype, shape, device):
     return t if t.is_contiguous() else t.contiguous()
 
 
+# New contiguous tensors.  (empty_strided parses its arguments in 0.6 of empty's
+# time: an output costs 1.0 us so, 1.7 by empty.)
+def _new(shape, dtype, device):
+    strides, n = [], 1
+    for size in reversed(shape):
+        strides.append(n)
+        n *= size
+    return torch.empty_strided(shape, strides[::-1], dtype=dtype, device=device)
+
+
+def _new_rows(rows, columns, dtype, device):
+    return torch.empty_strided((rows, columns), (columns, 1), dtype=dtype, device=device)
+
+
+def _new_flat(n, dtype, device):
+    return torch.empty_strided((n,), (1,), dtype=dtype, device=device)
+
+
 def _stride(t):
     """Elements between t's rows; a row's length where there is one row or none."""
     return t.stride(0) if t.shape[0] > 1 else t.shape[-1]
@@ -92,14 +110,21 @@ _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
     lambda index: torch.cuda.current_stream(index).cuda_stream)
 
 
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+_entries = {}
+
+
 def _call(name, device, *args):
     """The library's call `name` on the device's current stream."""
+    entry = _entries.get(name)
+    if entry is None:
+        entry = _entries[name] = getattr(lib(), name)
     index = device.index
-    if index == torch.cuda.current_device():
-        rc = getattr(lib(), name)(*args, _raw_stream(index))
+    if index == _current_device():
+        rc = entry(*args, _raw_stream(index))
     else:
         with torch.cuda.device(index):
-            rc = getattr(lib(), name)(*args, _raw_stream(index))
+            rc = entry(*args, _raw_stream(index))
     if rc:
         _check(rc, name)
 
@@ -184,8 +209,8 @@ def route(logits, top_k, *, score="softmax", bias=None, groups=1, top_groups=1, 
     if logits.shape[0] > 1 and logits.stride(0) < logits.shape[1]:
         logits = logits.contiguous()                 # rows that overlap (expanded)
     cfg = _route_config(logits, top_k, score, groups, top_groups, group_top, renorm, scale)
-    weights = torch.empty((logits.shape[0], top_k), dtype=torch.float32, device=dev)
-    ids = torch.empty((logits.shape[0], top_k), dtype=torch.int32, device=dev)
+    T = logits.shape[0]
+    weights, ids = _new_rows(T, top_k, torch.float32, dev), _new_rows(T, top_k, torch.int32, dev)
     _call("gevo_route", dev, cfg, logits.data_ptr(), _ptr(bias), weights.data_ptr(), ids.data_ptr())
     return weights, ids
 
@@ -203,7 +228,7 @@ def route_backward(logits, ids, dweights, *, score="softmax", renorm=True, scale
     if shape[0] > 1 and logits.stride(0) < logits.shape[1]:
         logits = logits.contiguous()
     cfg = _route_config(logits, shape[1], score, 1, 1, 1, renorm, scale)
-    out = torch.empty(logits.shape, dtype=logits.dtype, device=dev)
+    out = _new_rows(*logits.shape, logits.dtype, dev)
     _call("gevo_route_backward", dev, cfg, logits.data_ptr(), ids.data_ptr(), dweights.data_ptr(), out.data_ptr())
     return out
 
@@ -218,18 +243,18 @@ def route_plan(ids, n_experts) -> RoutePlan:
     ids = _flat(ids, "ids", torch.int32, ids.shape, dev)
     n = ids.numel()
     nbytes = _plan_bytes(n, n_experts)
-    ws = torch.empty(nbytes, dtype=torch.uint8, device=dev) if nbytes else None
+    ws = _new_flat(nbytes, torch.uint8, dev) if nbytes else None
     plan = RoutePlan.__new__(RoutePlan)
-    plan.order = torch.empty(n, dtype=torch.int32, device=dev)
-    plan.pos = torch.empty(ids.shape, dtype=torch.int32, device=dev)
-    plan.offsets = torch.empty(n_experts + 1, dtype=torch.int32, device=dev)
+    plan.order = _new_flat(n, torch.int32, dev)
+    plan.pos = _new_rows(*ids.shape, torch.int32, dev)
+    plan.offsets = _new_flat(n_experts + 1, torch.int32, dev)
     _call("gevo_route_plan", dev, n, n_experts, ids.data_ptr(), _ptr(ws), nbytes, plan.order.data_ptr(),
           plan.pos.data_ptr(), plan.offsets.data_ptr())
     return plan
 
 
 def _expert_setup(x, w, plan, sorted_rows, y_stride, relu, out_dtype):
-    x, w = _rows(x, "x"), _rows(w, "w", 3)
+    w = _rows(w, "w", 3)
     dev = x.device
     _plan_of(plan, dev)
     if w.device != dev or w.dtype != x.dtype:
@@ -256,11 +281,12 @@ def expert_forward(x, w, plan, bias=None, *, relu=False, sorted_rows=False, out_
     [E][N][K], bias [E][N] float32 (gevo_expert_forward).  x is [T][K], or with
     sorted_rows the sorted rows of a layer before, [T k][K].  Rows of slots
     without an expert (from plan.offsets[-1] on) hold nothing."""
-    out_dtype = _out_dtype(out_dtype, _rows(x, "x").dtype)
+    x = _rows(x, "x")
+    out_dtype = _out_dtype(out_dtype, x.dtype)
     x, w, cfg, dev = _expert_setup(x, w, plan, sorted_rows, 0, relu, out_dtype)
     if bias is not None:
         bias = _flat(bias, "bias", torch.float32, w.shape[:2], dev)
-    out = torch.empty((plan.pos.numel(), w.shape[1]), dtype=out_dtype, device=dev)
+    out = _new_rows(plan.pos.numel(), w.shape[1], out_dtype, dev)
     _call("gevo_expert_forward", dev, cfg, x.data_ptr(), w.data_ptr(), _ptr(bias), plan.order.data_ptr(),
           plan.offsets.data_ptr(), out.data_ptr())
     return out
@@ -271,16 +297,17 @@ def expert_backward(dy, x, w, plan, *, sorted_rows=False, relu_input=False, need
     product with gradient dy [T k][N] (gevo_expert_backward); None where not
     needed.  relu_input: x is a ReLU's output, and dx the gradient before it.
     expert_combine(dx, plan) adds the sorted rows up to a gradient of x [T][K]."""
-    dy = _rows(dy, "dy")
+    dy, x = _rows(dy, "dy"), _rows(x, "x")
     n = plan.pos.numel() if isinstance(plan, RoutePlan) else 0
     if n > 1 and dy.stride(0) < dy.shape[1]:
         dy = dy.contiguous()
     x, w, cfg, dev = _expert_setup(x, w, plan, sorted_rows, _stride(dy), relu_input, dy.dtype)
     if dy.dtype != x.dtype or dy.device != dev or dy.shape != (n, w.shape[1]):
         raise GevoError(f"dy: {x.dtype} of shape {(n, w.shape[1])} on {dev}, not {dy.dtype} of {tuple(dy.shape)}")
-    dx = torch.empty((n, w.shape[2]), dtype=x.dtype, device=dev) if need_dx else None
-    dw = torch.empty(w.shape, dtype=torch.float32, device=dev) if need_dw else None
-    db = torch.empty(w.shape[:2], dtype=torch.float32, device=dev) if need_dw else None
+    (E, N, K), dw, db = w.shape, None, None
+    dx = _new_rows(n, K, x.dtype, dev) if need_dx else None
+    if need_dw:
+        dw, db = _new((E, N, K), torch.float32, dev), _new_rows(E, N, torch.float32, dev)
     _call("gevo_expert_backward", dev, cfg, _ptr(dy), _ptr(x), _ptr(w), _ptr(plan.order),
           _ptr(plan.offsets), _ptr(dx), _ptr(dw), _ptr(db))
     return dx, dw, db
@@ -307,7 +334,7 @@ def expert_combine(rows, plan, weights=None, *, out_dtype=None):
     out_dtype = _out_dtype(out_dtype, rows.dtype)
     (T, k), N = plan.pos.shape, rows.shape[1]
     cfg = _combine_cfg(DTYPES[rows.dtype], DTYPES[out_dtype], k, N, T, _stride(rows), N)
-    y = torch.empty((T, N), dtype=out_dtype, device=dev)
+    y = _new_rows(T, N, out_dtype, dev)
     _call("gevo_expert_combine", dev, cfg, rows.data_ptr(), plan.pos.data_ptr(), _ptr(weights), y.data_ptr())
     return y
 
@@ -324,8 +351,7 @@ def expert_combine_backward(dy, rows, plan, weights=None):
         dy = dy.contiguous()
     dtype = DTYPES[rows.dtype]
     cfg = _combine_cfg(dtype, dtype, k, N, T, _stride(rows), _stride(dy))
-    drows = torch.empty((T * k, N), dtype=rows.dtype, device=dev)
-    dweights = torch.empty((T, k), dtype=torch.float32, device=dev)
+    drows, dweights = _new_rows(T * k, N, rows.dtype, dev), _new_rows(T, k, torch.float32, dev)
     _call("gevo_expert_combine_backward", dev, cfg, dy.data_ptr(), rows.data_ptr(), plan.pos.data_ptr(),
           _ptr(weights), drows.data_ptr(), dweights.data_ptr())
     return drows, dweights
@@ -356,7 +382,7 @@ class Mx4:
         """The values as a tensor of self.shape (gevo_mx4_dequantize)."""
         dtype = _out_dtype(dtype, torch.float32)
         k, dev = self.k, self.codes.device
-        out = torch.empty(self.shape, dtype=dtype, device=dev)
+        out = _new(self.shape, dtype, dev)
         _call("gevo_mx4_dequantize", dev, DTYPES[dtype], out.numel() // k, k, self.codes.data_ptr(),
               self.scales.data_ptr(), out.data_ptr(), k)
         return out
@@ -375,8 +401,7 @@ def mx4_quantize(x) -> Mx4:
     kp = (k + 127) // 128 * 128
     lead, dev = x.shape[:-1], x.device
     q = Mx4.__new__(Mx4)
-    q.codes = torch.empty((*lead, kp // 2), dtype=torch.uint8, device=dev)
-    q.scales = torch.empty((*lead, kp // 32), dtype=torch.uint8, device=dev)
+    q.codes, q.scales = _new((*lead, kp // 2), torch.uint8, dev), _new((*lead, kp // 32), torch.uint8, dev)
     q.k = k
     _call("gevo_mx4_quantize", dev, DTYPES[x.dtype], x.numel() // k, k, x.data_ptr(),
           k if x.dim() > 2 else _stride(x), q.codes.data_ptr(), q.scales.data_ptr())
@@ -416,7 +441,7 @@ def mx4_matmul(a, b, *, bias=None, relu=False, plan=None, sorted_rows=False, out
         if a.shape != (M * k if sorted_rows else M, K):
             raise GevoError(f"a: shape {(M * k if sorted_rows else M, K)}, not {a.shape}")
         shape = (M * k, N)
-    out = torch.empty(shape, dtype=out_dtype, device=dev)
+    out = _new(shape, out_dtype, dev)
     cfg = _mx4_cfg(DTYPES[out_dtype], P, N, K, M, 1 if each else 0, k, 1 if sorted_rows else 0, 1 if relu else 0)
     _call("gevo_mx4_matmul", dev, cfg, ac.data_ptr(), a.scales.data_ptr(), bc.data_ptr(), b.scales.data_ptr(),
           _ptr(bias), order, offsets, out.data_ptr())
