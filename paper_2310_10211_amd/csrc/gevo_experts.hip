@@ -851,6 +851,9 @@ __global__ __launch_bounds__(SH::kThreads, SH::WGS* SH::kThreads / 256) void k_e
   if (has_rows) {
     char* stage = smem + wu * 32 * kRowB;
     const float least = PASS == kForward && a.relu ? 0.0f : -INFINITY;
+    // all of the wave's part of the output exists and its chunks lie on 16 bytes
+    const bool filled = whole && !(PASS == kDx && a.mask) && tl.m0 + (wm + 1) * 32 * MI <= rows &&
+                        n0 + (wn + 1) * 32 * NI <= cols;
     // the lane's row and column in the first of the band's rounds
     const int64_t r0 = tl.m0 + wm * 32 * MI + lane / kCh;
     const int c0 = n0 + wn * 32 * NI + lane % kCh * kEl;
@@ -868,7 +871,7 @@ __global__ __launch_bounds__(SH::kThreads, SH::WGS* SH::kThreads / 256) void k_e
             for (int u = 0; u < 4; ++u) f[u] = acc[i][t][4 * q + u];
             if constexpr (PASS == kForward) {
 #pragma unroll
-              for (int u = 0; u < 4; ++u) f[u] = f[u] < least ? least : f[u];   // (NaN stays)
+              for (int u = 0; u < 4; ++u) f[u] = __builtin_elementwise_maximum(f[u], least);   // (NaN stays)
             }
             char* row = stage + l32 * kRowB;
             if constexpr (OUT16) {                 // chunk 4 t + q, half lh
@@ -880,6 +883,19 @@ __global__ __launch_bounds__(SH::kThreads, SH::WGS* SH::kThreads / 256) void k_e
             }
           }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        if (filled) {                              // no lane looks at what exists
+          uint4 u[kCh / 2];
+#pragma unroll
+          for (int j = 0; j < kCh / 2; ++j) {
+            const int rr = j * (64 / kCh) + lane / kCh;
+            u[j] = *reinterpret_cast<const uint4*>(stage + rr * kRowB + 16 * (lane % kCh ^ (rr & (kCh - 1))));
+          }
+#pragma unroll
+          for (int j = 0; j < kCh / 2; ++j)
+            *reinterpret_cast<uint4*>(o0 + ((32 * i + j * (64 / kCh)) * a.out_stride + 32 * t0)) = u[j];
+          __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+          continue;
+        }
 #pragma unroll
         for (int j = 0; j < kCh / 2; ++j) {        // 64 / kCh rows an instruction
           const int rr = j * (64 / kCh) + lane / kCh, ch = lane % kCh;
