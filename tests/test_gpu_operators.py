@@ -597,3 +597,74 @@ def test_refused_sizes():
                  lambda: g.mx4_quantize(torch.empty(1, 1, device="cuda").expand(0, big + 128))):
         with pytest.raises(g.GevoError):
             call()
+
+
+# ------------------------------------------------- many row tiles, full steps
+@pytest.mark.parametrize("T,k,E,N,K,dtype", [(2500, 1, 1, 700, 192, "bf16"), (2700, 3, 2, 300, 128, "f32"),
+                                             (5000, 2, 3, 520, 200, "bf16"), (2300, 7, 5, 66, 256, "bf16")])
+def test_experts_of_more_than_eight_row_tiles(T, k, E, N, K, dtype):
+    """Tiles are taken eight rows of them at a time: every one once, at both ends of a group."""
+    gen, ids, plan = _routed(T, k, E, 11)
+    x, w, dy = _randn(gen, T, K, dtype=dtype), _randn(gen, E, N, K, dtype=dtype), _randn(gen, T * k, N, dtype=dtype)
+    order, _, off = ref.plan(ids.cpu().numpy(), E)
+    n = off[-1]
+    y = g.expert_forward(x, w, plan, out_dtype=torch.float32)
+    want, mag = ref.expert_rows(_np(x), _np(w), None, order, off, k)
+    _close(_np(y)[:n], want, mag, K, "f32")
+    got = g.expert_backward(dy, x, w, plan)
+    want, mag = ref.expert_grads(_np(dy), _np(x), _np(w), order, off, k)
+    most = int(np.max(off[1:] - off[:-1]))
+    for a, b, m, c, d in zip(got, want, mag, (N, most, most), (dtype, "f32", "f32")):
+        _close(_np(a)[:len(b)], b, m, c, d)
+
+
+@pytest.mark.parametrize("P,M,N,K,each", [(2, 2500, 300, 512, False), (2, 2500, 300, 512, True), (1, 5000, 270, 768, False)])
+def test_mx4_matmul_of_more_than_eight_row_tiles(P, M, N, K, each):
+    gen = _rng("mx4 rows", P, M, each)
+    a, b = g.mx4_quantize(_randn(gen, *((P, M, K) if each else (M, K)))), g.mx4_quantize(_randn(gen, P, N, K))
+    av, bv = _np(a.dequantize()), _np(b.dequantize())
+    y = g.mx4_matmul(a, b)
+    _close(_np(y), av @ bv.transpose(0, 2, 1), np.abs(av) @ np.abs(bv).transpose(0, 2, 1), K, "f32")
+
+
+@pytest.mark.parametrize("dtype,K", [("f32", 96), ("bf16", 192), ("bf16", 200)])
+def test_rows_outside_x_read_zeros(dtype, K):
+    """A sorted row whose slot no row of x has is a row of zeros: its output the bias, its part of dw nothing."""
+    T, k, E, N = 300, 3, 2, 140
+    gen, ids, plan = _routed(T, k, E, 12, some_missing=False)
+    order = plan.order.clone()
+    gone = torch.tensor([0, 5, 130, 131, 500, T * k - 1], device="cuda")
+    order[gone] = torch.tensor([T * k, -1, 1 << 30, T * k + 7, -5, (1 << 31) - 1], dtype=torch.int32, device="cuda")
+    odd = g.RoutePlan(order, plan.pos, plan.offsets)
+    x, w, b = _randn(gen, T, K, dtype=dtype), _randn(gen, E, N, K, dtype=dtype), _randn(gen, E, N)
+    y, whole = (g.expert_forward(x, w, p, b, out_dtype=torch.float32) for p in (odd, plan))
+    expert = torch.searchsorted(plan.offsets[1:].contiguous(), gone.int(), right=True)
+    assert torch.equal(y[gone], b[expert])
+    keep = torch.ones(T * k, dtype=torch.bool, device="cuda")
+    keep[gone] = False
+    assert torch.equal(y[keep], whole[keep])
+    dy = _randn(gen, T * k, N, dtype=dtype)
+    dy0 = dy.clone()
+    dy0[gone] = 0
+    got, want = (g.expert_backward(d, x, w, p, need_dx=False)[1] for d, p in ((dy, odd), (dy0, plan)))
+    # the same products, and zeros, in the same order
+    assert torch.equal(got, want)
+
+
+def test_offsets_past_32_bits_in_tiles():
+    """The last of three experts lies more than 4 GB into the weights, rows enough for tiles."""
+    E, N, K, T = 3, 16400, 65600, 300
+    w = torch.zeros(E, N, K, dtype=torch.bfloat16, device="cuda")
+    w[2, N - 300:] = torch.randn(300, K, device="cuda").bfloat16()
+    x = torch.randn(T, K, device="cuda").bfloat16()
+    plan = g.route_plan(torch.full((T, 1), 2, dtype=torch.int32, device="cuda"), E)
+    y = g.expert_forward(x, w, plan, out_dtype=torch.float32)
+    xs, ws = x.double(), w[2, N - 300:].double()
+    _close(_np(y)[:, N - 300:], _np(xs @ ws.T), _np(xs.abs() @ ws.abs().T), K, "f32")
+    assert (y[:, :N - 300] == 0).all()
+    dy = torch.randn(T, N, device="cuda").bfloat16()
+    dx = g.expert_backward(dy, x, w, plan, need_dw=False)[0]
+    ds = dy[:, N - 300:].double()
+    _close(_np(dx), _np(ds @ ws), _np(ds.abs() @ ws.abs()), N, "bf16")
+    del w, dx
+    torch.cuda.empty_cache()
