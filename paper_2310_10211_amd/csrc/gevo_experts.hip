@@ -212,8 +212,8 @@ __device__ __forceinline__ bool find_tile(const ExpertArgs& a, int ntiles, Tile&
   if (!a.offsets) {
     // Every matrix's rows are the same: an eighth of the row tiles goes to each
     // XCD for all matrices, so that these rows stay in its L2 and the matrices
-    // pass by (64 variants of 784-512 over 10,000 rows in 4 bits 327 us;
-    // an eighth of the matrices to each XCD, as where rows differ, 343).
+    // pass by (64 variants of 784-512 over 10,000 rows in 4 bits: an eighth of
+    // the matrices to each XCD, as where rows differ, takes 5% longer).
     const uint32_t rts = (uint32_t)((a.M + kXR - 1) / kXR), all = (uint32_t)a.E * (uint32_t)ntiles;
     const Place in = grouped(idx, rts, all, a.x_e == 0 ? max(1u, min(8u, (rts + 7) / 8)) : 8);
     const uint32_t c = (uint32_t)__builtin_amdgcn_readfirstlane((int)in.col);
@@ -487,7 +487,7 @@ __global__ __launch_bounds__(SH::kThreads, SH::WGS* SH::kThreads / 256) void k_e
   };
   // The same where step st lies inside every operand and no row is out of place:
   // an address a load, without a look at what exists (which took 30 instructions
-  // a load: 8,192 rows through 4 of 64 experts of 2048 x 2048 434 us, so 419).
+  // a load: 8,192 rows through 4 of 64 experts of 2048 x 2048 3% longer).
   // Rows and columns outside the operands read the first ones, and their products
   // are not written.
   const bool plain = kAllDma && __all(there);

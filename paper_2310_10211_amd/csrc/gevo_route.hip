@@ -84,17 +84,19 @@ __device__ __forceinline__ double unordered(double f) { return f; }
 // L lanes share a row, each holding NE consecutive logits.  A choice is the
 // row's largest local maximum and the lowest index that holds it, taken out by
 // the lane that has it.  Keys in 32 bits are compared as integers that order
-// like them, whose maximum of three is one instruction.  Bound by these
-// instructions (65,536 rows of 256, 8 groups, 8 chosen: 60 us, of which their
-// bytes take 13; 68 with keys compared as floats; finding the k-th key by
-// bisection took as long, a row in a whole wave 135).
+// like them, whose maximum of three is one instruction, with their place in the
+// lane in the low bits, which finds and removes a key in three instructions.
+// Bound by instructions and their latency: 65,536 rows of 256, 8 groups, 8
+// chosen take 50 us, of which their bytes take 14 (60 with logits and biases
+// held in registers through the choice, five waves a SIMD where it is six now;
+// finding the k-th key by bisection took as long, a row in a whole wave 135).
 //
 // Two keys nearer than the rounding of 32-bit scores would be ordered by that
 // rounding: a row with such a pair among the keys (or groups) that decide its
 // choice is done over with 64-bit keys, which a wave does when one of its rows
 // asks for it.  Logits as keys need none of this.
 template <typename S, int L, int NE>
-__global__ __launch_bounds__(256) void k_route(RouteArgs a) {
+__global__ __launch_bounds__(256, NE == 16 ? 6 : 1) void k_route(RouteArgs a) {
   constexpr int kRows = 256 / L;
   extern __shared__ __align__(16) char smem[];
   const int lane = threadIdx.x & (L - 1), rw = threadIdx.x / L;
@@ -104,20 +106,37 @@ __global__ __launch_bounds__(256) void k_route(RouteArgs a) {
   const int e0 = lane * NE;
   const float ninf = -INFINITY;
 
-  float l[NE];
-  if (a.vec) {                                       // whole rows of aligned chunks
-    constexpr int V = 16 / sizeof(S) < NE ? 16 / sizeof(S) : NE;
+  // Logits and biases are read again where the rarer paths want them, rather than
+  // held through the choice: 16 of each are a third of its registers.
+  float l[NE], b[NE];                                // (biases past the row's end: any of its values)
+  auto load_logits = [&]() {
+    if (a.vec) {                                     // whole rows of aligned chunks
+      constexpr int V = 16 / sizeof(S) < NE ? 16 / sizeof(S) : NE;
 #pragma unroll
-    for (int j = 0; j < NE; j += V) {
-      S e[V];
-      __builtin_memcpy(e, __builtin_assume_aligned(lrow + e0 + j, V * sizeof(S)), sizeof(e));
+      for (int j = 0; j < NE; j += V) {
+        S e[V];
+        __builtin_memcpy(e, __builtin_assume_aligned(lrow + e0 + j, V * sizeof(S)), sizeof(e));
 #pragma unroll
-      for (int v = 0; v < V; ++v) l[j + v] = live ? to_f<S>(e[v]) : ninf;
+        for (int v = 0; v < V; ++v) l[j + v] = live ? to_f<S>(e[v]) : ninf;
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < NE; ++j) l[j] = live && e0 + j < a.E ? to_f<S>(lrow[e0 + j]) : ninf;
     }
-  } else {
+  };
+  auto load_biases = [&]() {
 #pragma unroll
-    for (int j = 0; j < NE; ++j) l[j] = live && e0 + j < a.E ? to_f<S>(lrow[e0 + j]) : ninf;
-  }
+    for (int j = 0; j < NE; ++j) b[j] = 0.0f;
+    if (!a.bias) return;
+    if (a.vec) {
+      __builtin_memcpy(b, a.bias + e0, sizeof(b));
+    } else {
+#pragma unroll
+      for (int j = 0; j < NE; ++j) b[j] = a.bias[e0 + j < a.E ? e0 + j : 0];
+    }
+  };
+  load_logits();
+  load_biases();
 
   bool bad = false;                                  // NaN, or +inf under softmax: no scores
   float m = ninf;
@@ -126,16 +145,8 @@ __global__ __launch_bounds__(256) void k_route(RouteArgs a) {
     bad |= __builtin_isunordered(l[j], l[j + 1]);
     m = fmaxf(fmaxf(l[j], l[j + 1]), m);
   }
-  float bmax = 0.0f, b[NE];                          // (past the row's end: any of its values)
-#pragma unroll
-  for (int j = 0; j < NE; ++j) b[j] = 0.0f;
+  float bmax = 0.0f;
   if (a.bias) {
-    if (a.vec) {
-      __builtin_memcpy(b, a.bias + e0, sizeof(b));
-    } else {
-#pragma unroll
-      for (int j = 0; j < NE; ++j) b[j] = a.bias[e0 + j < a.E ? e0 + j : 0];
-    }
 #pragma unroll
     for (int j = 0; j < NE; j += 2) {
       bad |= __builtin_isunordered(b[j], b[j + 1]);
@@ -165,6 +176,10 @@ __global__ __launch_bounds__(256) void k_route(RouteArgs a) {
     auto less = [](K x, K y) { return x < y ? x : y; };
     K key[NE];
     F tol = 0;
+    if constexpr (wide) {
+      load_logits();
+      load_biases();
+    }
     if (a.by_logit) {
 #pragma unroll
       for (int j = 0; j < NE; ++j) key[j] = ordered((F)l[j] + (F)0);   // (-0 is 0)
@@ -263,29 +278,60 @@ __global__ __launch_bounds__(256) void k_route(RouteArgs a) {
       for (int j = 0; j < NE; j += 2) v = more(more(key[j], key[j + 1]), v);
       return v;
     };
-    K lm = largest();
     picked[rw][lane] = -1;
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     K last = lowest;
-    const int tries = wide || a.by_logit ? a.k : a.k + 1;   // the first key left out is looked at, too
-    for (int i = 0; i < tries; ++i) {
-      const K mx = row_reduce<L>(lm, more);
-      if (!wide && !a.by_logit && i > 0 && last > lowest && !(unordered(last) - unordered(mx) > tol)) sure = false;
-      if (i == a.k) break;
-      last = mx;
-      const uint64_t hold = row_ballot<L>(lm == mx && mx > lowest);
-      const bool owner = lane == __ffsll((unsigned long long)hold) - 1;
-      bool left = owner;                             // the first of its keys that is as large goes
-      int at = 0;
+    if constexpr (wide) {
+      K lm = largest();
+      for (int i = 0; i < a.k; ++i) {
+        const K mx = row_reduce<L>(lm, more);
+        const uint64_t hold = row_ballot<L>(lm == mx && mx > lowest);
+        const bool owner = lane == __ffsll((unsigned long long)hold) - 1;
+        bool left = owner;                           // the first of its keys that is as large goes
+        int at = 0;
 #pragma unroll
-      for (int j = 0; j < NE; ++j) {
-        const bool hit = left && key[j] == mx;
-        at = hit ? j : at;
-        key[j] = hit ? lowest : key[j];
-        left = left && !hit;
+        for (int j = 0; j < NE; ++j) {
+          const bool hit = left && key[j] == mx;
+          at = hit ? j : at;
+          key[j] = hit ? lowest : key[j];
+          left = left && !hit;
+        }
+        lm = largest();
+        if (owner) picked[rw][i] = e0 + at;
       }
-      lm = largest();
-      if (owner) picked[rw][i] = e0 + at;
+    } else {
+      // A key's low bits hold its place in the lane, the first the largest, so the
+      // lane's largest key is one of its own and says which.  Between lanes the
+      // rest of the keys is compared, which orders like the keys where it differs:
+      // for logits in bf16 it is all there is; other keys that agree in it are in
+      // doubt.  (Keys below `lowest` are -inf's.)
+      constexpr K low = NE - 1;
+      constexpr bool exact = sizeof(S) == 2;
+      const F cut = NE * 2.4e-7f;                    // of a key, what its low bits or its like's come to
+#pragma unroll
+      for (int j = 0; j < NE; ++j) key[j] = (key[j] & ~low) | (low - j);
+      K lm = largest();
+      const int tries = a.by_logit && exact ? a.k : a.k + 1;   // the first key left out is looked at, too
+      for (int i = 0; i < tries; ++i) {
+        const K mx = more(row_reduce<L>(lm & ~low, more), lowest);
+        if (last > lowest) {
+          if (!a.by_logit) {
+            const F x = unordered(last);
+            if (!(x - unordered(mx) > tol + cut * fabsf(x))) sure = false;
+          } else if (!exact && last == mx) {
+            sure = false;
+          }
+        }
+        if (i == a.k) break;
+        last = mx;
+        const uint64_t hold = row_ballot<L>((lm & ~low) == mx && mx > lowest);
+        const bool owner = lane == __ffsll((unsigned long long)hold) - 1;
+        if (owner) picked[rw][i] = e0 + (int)(low - (lm & low));
+        const K out = owner ? lm : 0x7fffffff;       // (no key)
+#pragma unroll
+        for (int j = 0; j < NE; ++j) key[j] = key[j] == out ? lowest : key[j];
+        lm = largest();
+      }
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     chosen = picked[rw][lane];
@@ -317,6 +363,7 @@ __global__ __launch_bounds__(256) void k_route(RouteArgs a) {
     w = 1.0f / (1.0f + expf(-lc)) * a.scale;
   } else {
     float sum = 0.0f;
+    load_logits();
 #pragma unroll
     for (int j = 0; j < NE; ++j) sum += l[j] == ninf ? 0.0f : exp_split(l[j] - m);
     sum = row_reduce<L>(sum, [](float x, float y) { return x + y; });

@@ -668,3 +668,25 @@ def test_offsets_past_32_bits_in_tiles():
     _close(_np(dx), _np(ds @ ws), _np(ds.abs() @ ws.abs()), N, "bf16")
     del w, dx
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("E,k,groups", [(64, 5, 1), (128, 8, 4), (256, 8, 8), (200, 20, 1), (512, 6, 1), (1000, 9, 8), (2048, 12, 1)])
+def test_route_of_logits_that_agree_or_nearly(dtype, E, k, groups):
+    """Equal logits in one lane and across lanes, and ones that differ in the last
+    bits of a binary32, of both signs: the choice is the exact one."""
+    gen = _rng("near logits", E)
+    few = torch.randint(-3, 4, (24, E), generator=gen, device="cuda").float()         # many ties
+    step = torch.randint(0, 40, (24, E), generator=gen, device="cuda").float()
+    near = few + torch.where(few == 0, step * 1e-30, few * step * 2.0 ** -23)         # within 40 steps of each
+    wide = _randn(gen, 24, E, by=3.0)
+    wide[:, :: 3] = float("-inf")
+    for l in (few, near, wide, near.abs(), -near.abs()):
+        how = dict(groups=groups, top_groups=max(1, groups // 2))
+        _check_route(l.to(DT[dtype]).contiguous(), k, how)
+        _check_route(l.to(DT[dtype]).contiguous(), k, dict(how, score="sigmoid", renorm=False))
+    bias = few[0] * 1e-3
+    for score in ("softmax", "sigmoid"):
+        _check_route(near[:6].to(DT[dtype]).contiguous(), k, dict(score=score, bias=bias, groups=groups,
+                                                                  top_groups=max(1, groups // 2), group_top=2))
+        _check_route(wide[:6].to(DT[dtype]).contiguous(), k, dict(score=score, bias=bias - 5.0))
