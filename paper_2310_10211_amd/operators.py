@@ -195,6 +195,8 @@ def _route_config(logits, k, score, groups, top_groups, group_top, renorm, scale
     if min(k, groups, top_groups, group_top) < 1:
         raise GevoError("top_k, groups, top_groups and group_top: at least 1")
     T, E = logits.shape
+    if k > E:
+        raise GevoError(f"top_k: at most the {E} experts, not {k}")
     return _route_cfg(E, k, T, DTYPES[logits.dtype], SCORES[score], _stride(logits) if T > 1 else E, groups,
                       top_groups, group_top, 1 if renorm else 0, scale)
 

@@ -690,3 +690,38 @@ def test_route_of_logits_that_agree_or_nearly(dtype, E, k, groups):
         _check_route(near[:6].to(DT[dtype]).contiguous(), k, dict(score=score, bias=bias, groups=groups,
                                                                   top_groups=max(1, groups // 2), group_top=2))
         _check_route(wide[:6].to(DT[dtype]).contiguous(), k, dict(score=score, bias=bias - 5.0))
+
+
+def test_more_choices_than_experts_are_refused_before_their_memory():
+    x = torch.zeros(4, 8, device="cuda")
+    for k in (9, 1 << 31, (1 << 32) - 1):
+        with pytest.raises(g.GevoError):
+            g.route(x, k)
+
+
+@pytest.mark.parametrize("T,E,N,K", [(3800, 1, 4096, 256), (9000, 2, 1100, 200)])
+def test_large_tiles_captured_and_replayed(T, E, N, K):
+    """Tiles whose memory on chip asks for an attribute of the kernel, inside a capture."""
+    gen = _rng("large graph", T)
+    x, w, dy = (_randn(gen, *s, dtype="bf16") for s in ((T, K), (E, N, K), (T, N)))
+    ids = torch.randint(0, E, (T, 1), generator=gen, device="cuda", dtype=torch.int32)
+
+    def both():
+        plan = g.route_plan(ids, E)
+        q = g.mx4_matmul(g.mx4_quantize(x), g.mx4_quantize(w), plan=plan, out_dtype=torch.bfloat16)
+        return (g.expert_forward(x, w, plan, relu=True), *g.expert_backward(dy, x, w, plan), q)
+    both()
+    torch.cuda.synchronize()
+    stream, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        outs = both()
+    for i in range(3):
+        for t in (x, w, dy):
+            t.copy_(_randn(gen, *t.shape, dtype="bf16"))
+        ids.copy_(torch.randint(0, E, (T, 1), generator=gen, device="cuda", dtype=torch.int32))
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(outs, both()):
+            assert torch.equal(a, b), i
+        torch.cuda.synchronize()
