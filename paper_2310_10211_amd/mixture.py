@@ -22,8 +22,8 @@ from __future__ import annotations
 import torch
 
 from . import BF16, GevoError, Population
-from .operators import (expert_combine, expert_combine_backward, expert_forward, mx4_matmul, mx4_quantize, route,
-                        route_backward, route_plan)
+from .operators import (_number, expert_combine, expert_combine_backward, expert_forward, mx4_matmul, mx4_quantize,
+                        route, route_backward, route_plan)
 
 
 class Mixture:
@@ -95,6 +95,8 @@ class Mixture:
         route's options.  state is what gate_gradient asks for."""
         if gate_logits.shape != (x.shape[0], self.n_variants):
             raise GevoError(f"gate_logits: shape {(x.shape[0], self.n_variants)}, not {tuple(gate_logits.shape)}")
+        if "scale" in how:                           # its value now, which the gradient takes too
+            how["scale"] = _number("scale", how["scale"])
         weights, ids = route(gate_logits, top_k, **how)
         plan = route_plan(ids, self.n_variants)
         rows = self.rows_of(x, plan)

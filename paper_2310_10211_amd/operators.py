@@ -22,6 +22,7 @@ from __future__ import annotations
 
 import ctypes
 import functools
+import operator
 
 import torch
 
@@ -100,7 +101,7 @@ def _stride(t):
 def _out_dtype(dtype, default):
     if dtype is None:
         return default
-    if dtype not in DTYPES:
+    if not isinstance(dtype, torch.dtype) or dtype not in DTYPES:
         raise GevoError(f"out_dtype: float32 or bfloat16, not {dtype}")
     return dtype
 
@@ -140,8 +141,28 @@ def _u32_ok(name, value):
     return value
 
 
-# The configurations of calls, by their values: a program repeats a few, and the
-# library reads them during the call alone.
+# Numbers of the caller's as plain ones, read at the call: a tensor or an array
+# of one value can change, and would be kept by its identity below.
+def _index(name, value):
+    if type(value) is int:
+        return value
+    try:
+        return operator.index(value)
+    except (TypeError, ValueError, RuntimeError):
+        raise GevoError(f"{name}: an integer, not {value!r}") from None
+
+
+def _number(name, value):
+    if type(value) is not float:
+        try:
+            value = ctypes.c_float(value).value
+        except (TypeError, ValueError, RuntimeError, OverflowError):
+            raise GevoError(f"{name}: a number, not {value!r}") from None
+    return value + 0.0                               # (-0 and 0 are one key)
+
+
+# The configurations of calls, by their values, which are plain numbers: a program
+# repeats a few, and the library reads them during the call alone.
 def _config(cls):
     def make(*values):
         for (name, kind), value in zip(cls._fields_[1:], values):
@@ -190,15 +211,17 @@ def _plan_of(plan, device):
 
 
 def _route_config(logits, k, score, groups, top_groups, group_top, renorm, scale):
-    if score not in SCORES:
+    if not isinstance(score, str) or score not in SCORES:
         raise GevoError(f"score: one of {sorted(SCORES)}, not {score!r}")
+    k, groups = _index("top_k", k), _index("groups", groups)
+    top_groups, group_top = _index("top_groups", top_groups), _index("group_top", group_top)
     if min(k, groups, top_groups, group_top) < 1:
         raise GevoError("top_k, groups, top_groups and group_top: at least 1")
     T, E = logits.shape
     if k > E:
         raise GevoError(f"top_k: at most the {E} experts, not {k}")
     return _route_cfg(E, k, T, DTYPES[logits.dtype], SCORES[score], _stride(logits) if T > 1 else E, groups,
-                      top_groups, group_top, 1 if renorm else 0, scale)
+                      top_groups, group_top, 1 if renorm else 0, _number("scale", scale))
 
 
 def route(logits, top_k, *, score="softmax", bias=None, groups=1, top_groups=1, group_top=1, renorm=True, scale=1.0):
@@ -210,6 +233,7 @@ def route(logits, top_k, *, score="softmax", bias=None, groups=1, top_groups=1, 
         bias = _flat(bias, "bias", torch.float32, logits.shape[1:], dev)
     if logits.shape[0] > 1 and logits.stride(0) < logits.shape[1]:
         logits = logits.contiguous()                 # rows that overlap (expanded)
+    top_k = _index("top_k", top_k)
     cfg = _route_config(logits, top_k, score, groups, top_groups, group_top, renorm, scale)
     T = logits.shape[0]
     weights, ids = _new_rows(T, top_k, torch.float32, dev), _new_rows(T, top_k, torch.int32, dev)
@@ -239,6 +263,7 @@ def route_plan(ids, n_experts) -> RoutePlan:
     """The slots of ids [T][k] sorted by expert (gevo_route_plan)."""
     if not (isinstance(ids, torch.Tensor) and ids.is_cuda and ids.dim() == 2):
         raise GevoError("ids: a tensor [T][k] on the GPU")
+    n_experts = _index("n_experts", n_experts)
     if n_experts < 1:
         raise GevoError("n_experts: at least 1")
     dev = ids.device
@@ -367,6 +392,7 @@ class Mx4:
     __slots__ = ("codes", "scales", "k")
 
     def __init__(self, codes, scales, k):
+        k = _index("k", k)
         if not (1 <= k < 1 << 32 and isinstance(codes, torch.Tensor) and codes.is_cuda and codes.dim() >= 2):
             raise GevoError("codes: a tensor [..., rows, Kp / 2] on the GPU")
         kp = (k + 127) // 128 * 128

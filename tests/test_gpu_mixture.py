@@ -202,3 +202,17 @@ def test_mixture_refusals():
         with pytest.raises(g.GevoError):
             call()
     pop.close()
+
+
+def test_the_gates_gradient_takes_the_predictions_scale():
+    """A scale changed after predict is not the one that its state's gradient is of."""
+    pop = _population([40, 10], 5, "f32")
+    m, x = Mixture(pop), pop.x_test
+    gate = torch.randn(len(x), 5, generator=torch.Generator("cuda").manual_seed(7), device="cuda")
+    dl = torch.randn(len(x), 10, generator=torch.Generator("cuda").manual_seed(8), device="cuda")
+    scale = torch.tensor(1.5)
+    _, state = m.predict(x, gate, 2, scale=scale)
+    scale.fill_(4.0)
+    want = Mixture.gate_gradient(m.predict(x, gate, 2, scale=1.5)[1], dl)
+    assert torch.equal(Mixture.gate_gradient(state, dl), want)
+    pop.close()

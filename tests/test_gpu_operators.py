@@ -725,3 +725,19 @@ def test_large_tiles_captured_and_replayed(T, E, N, K):
         for a, b in zip(outs, both()):
             assert torch.equal(a, b), i
         torch.cuda.synchronize()
+
+
+def test_a_scale_that_changes_in_place():
+    """A tensor's value is read at each call: a scale is not kept by its identity."""
+    x = torch.randn(6, 9, device="cuda")
+    dw = torch.randn(6, 2, device="cuda")
+    for t in (torch.tensor(2.5), torch.tensor([2.5]), np.array(2.5)):
+        for value in (2.5, 5.0, -0.0):
+            t[...] = value
+            w, ids = g.route(x, 2, scale=t)
+            assert torch.equal(w, g.route(x, 2, scale=float(value))[0])
+            assert torch.equal(g.route_backward(x, ids, dw, scale=t), g.route_backward(x, ids, dw, scale=float(value)))
+    n = torch.tensor(9)
+    a = g.route_plan(ids, n)
+    n += 3
+    assert a.n_experts == 9 and g.route_plan(ids, n).n_experts == 12

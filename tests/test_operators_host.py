@@ -176,6 +176,54 @@ def test_sizes_past_32_bits_are_refused():
     assert o._route_cfg(8, 2, 4, 0, 0, 8, 1, 1, 1, 1, 1.0) is not None
 
 
+def _route_config(scale=1.0, k=2, score="softmax", groups=1, top_groups=1, group_top=1):
+    import torch
+    from paper_2310_10211_amd import operators as o
+    return o._route_config(torch.zeros(3, 8), k, score, groups, top_groups, group_top, True, scale)._obj
+
+
+def test_configurations_hold_values_not_objects():
+    """A tensor or an array that changes in place changes the next call."""
+    import torch
+    from paper_2310_10211_amd import operators as o
+    _lib()
+    for t in (torch.tensor(2.5), torch.tensor([2.5], dtype=torch.float64), np.array(2.5), np.float32(2.5)):
+        assert _route_config(t).scale == 2.5
+    t, a = torch.tensor(2.5), np.array(2.5)
+    for value in (5.0, 0.0, -1.25):
+        t.fill_(value)
+        a[...] = value
+        assert _route_config(t).scale == value and _route_config(a).scale == value
+    k = torch.tensor(2)
+    assert _route_config(k=k).k == 2
+    k += 1
+    assert _route_config(k=k).k == 3 and _route_config(k=np.int64(3)).k == 3 and _route_config(groups=np.int32(4)).groups == 4
+    assert math.copysign(1, _route_config(0.0).scale) == math.copysign(1, _route_config(-0.0).scale)
+    assert o._number("scale", 2) == 2.0 and o._index("k", True) == 1
+
+
+def test_what_is_no_number_is_refused():
+    import torch
+    _lib()
+    x = torch.zeros(2, 4)
+    for bad in ([2.5], "2.5", None, np.zeros(2), torch.zeros(2), 1j, {}, 10 ** 400):
+        with pytest.raises(g.GevoError):
+            _route_config(bad)
+    for bad in (2.0, "2", None, [2], np.zeros(2, int), torch.tensor(2.0)):
+        for name in ("k", "groups", "top_groups", "group_top"):
+            with pytest.raises(g.GevoError):
+                _route_config(**{name: bad})
+        with pytest.raises(g.GevoError):
+            g.Mx4(x, x, bad)
+    for bad in (["softmax"], None, 0, {}):
+        with pytest.raises(g.GevoError):
+            _route_config(score=bad)
+    from paper_2310_10211_amd import operators as o
+    for bad in ([], "float32", 0):
+        with pytest.raises(g.GevoError):
+            o._out_dtype(bad, torch.float32)
+
+
 # ------------------------------------------------------------- the oracle itself
 def test_oracle_route_closed_forms():
     l = [math.log(4), math.log(1), math.log(3), -math.inf]
