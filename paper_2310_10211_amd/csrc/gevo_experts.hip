@@ -1037,7 +1037,7 @@ __global__ __launch_bounds__(256, 4) void k_expert_few(ExpertArgs a) {
       __syncthreads();
       acc = part[0][lane] + part[1][lane] + part[2][lane] + part[3][lane];
     }
-    if ((!SPLIT || wave == 0) && r >= 0) {           // lane: row l16, columns n0 + 4 lk + 0 .. 3
+    if ((!SPLIT || wave == 0) && i < cnt) {          // lane: row l16, columns n0 + 4 lk + 0 .. 3
 #pragma unroll
       for (int u = 0; u < 4; ++u) {
         const int c = n0 + 4 * lk + u;

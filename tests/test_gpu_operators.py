@@ -741,3 +741,35 @@ def test_a_scale_that_changes_in_place():
     a = g.route_plan(ids, n)
     n += 3
     assert a.n_experts == 9 and g.route_plan(ids, n).n_experts == 12
+
+
+def _odd_plan(plan, T, k, gone):
+    """The plan with `gone` of its sorted rows naming slots that no row of x has."""
+    order = plan.order.clone()
+    names = [T * k, -1, 1 << 30, (1 << 31) - 1, -(1 << 31), T * k + 7]
+    order[gone] = torch.tensor([names[i % len(names)] for i in range(len(gone))], dtype=torch.int32, device="cuda")
+    keep = torch.ones(T * k, dtype=torch.bool, device="cuda")
+    keep[gone] = False
+    return g.RoutePlan(order, plan.pos, plan.offsets), keep
+
+
+@pytest.mark.parametrize("kind", ["f32", "bf16", "mx4"])
+@pytest.mark.parametrize("T,k,E,N,K", [(20, 2, 5, 40, 96), (20, 2, 5, 33, 2100), (9, 1, 9, 16, 1027), (30, 3, 2, 70, 4)])
+def test_few_rows_outside_x_read_zeros(kind, T, k, E, N, K):
+    """The same where an expert has few rows, the contraction split over waves and not."""
+    gen, ids, plan = _routed(T, k, E, 13, some_missing=False)
+    gone = torch.tensor([0, 1, T * k // 2, T * k - 1], device="cuda")
+    odd, keep = _odd_plan(plan, T, k, gone)
+    x, w, b = _randn(gen, T, K), _randn(gen, E, N, K), _randn(gen, E, N)
+    expert = torch.searchsorted(plan.offsets[1:].contiguous(), gone.int(), right=True)
+    if kind == "mx4":
+        xq, wq = g.mx4_quantize(x), g.mx4_quantize(w)
+        run = lambda p, **how: g.mx4_matmul(xq, wq, bias=b, plan=p, **how)                      # noqa: E731
+    else:
+        run = lambda p, **how: g.expert_forward(x.to(DT[kind]), w.to(DT[kind]), p, b, **how)    # noqa: E731
+    for relu in (False, True):
+        for out in (torch.float32, torch.bfloat16):
+            y, whole = (run(p, relu=relu, out_dtype=out) for p in (odd, plan))
+            want = b[expert].clamp(min=0) if relu else b[expert]
+            assert torch.equal(y[gone], want.to(out)), (relu, out)
+            assert torch.equal(y[keep], whole[keep])
