@@ -907,7 +907,8 @@ __global__ __launch_bounds__(SH::kThreads, SH::WGS* SH::kThreads / 256) void k_e
             if (a.mask) {
               const int64_t mr = placed_row(a, a.mask_order, a.mask_rows, tl.s0 + r);
               const char* mp = (const char*)a.mask + (mr < 0 ? 0 : mr) * a.mask_stride + (size_t)c * sizeof(S);
-              const uint4 mu = load_chunk<S>(mp, cols - c, n0 + kWR > cols, cols >= V, (const char*)a.mask);
+              const uint4 mu =               // (a row outside x: zeros)
+                  load_chunk<S>(mp, mr < 0 ? 0 : cols - c, n0 + kWR > cols, cols >= V, (const char*)a.mask);
               S me[V];
               O oe[kEl];
               static_assert(PASS != kDx || V == kEl, "dx has its input's type");

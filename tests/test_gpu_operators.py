@@ -773,3 +773,20 @@ def test_few_rows_outside_x_read_zeros(kind, T, k, E, N, K):
             want = b[expert].clamp(min=0) if relu else b[expert]
             assert torch.equal(y[gone], want.to(out)), (relu, out)
             assert torch.equal(y[keep], whole[keep])
+
+
+@pytest.mark.parametrize("dtype,K", [("f32", 96), ("f32", 3), ("bf16", 192), ("bf16", 200), ("bf16", 67)])
+@pytest.mark.parametrize("T", [9, 300])
+def test_a_row_outside_x_clears_its_gradient(dtype, K, T):
+    """With relu_input a sorted row whose slot no row of x has was a row of zeros, of
+    which none is > 0; row 0 of x, which lets everything pass, has no part in it."""
+    k, E, N = 3, 2, 140
+    gen, ids, plan = _routed(T, k, E, 14, some_missing=False)
+    gone = torch.tensor([0, 3, T * k // 2, T * k - 1], device="cuda")
+    odd, keep = _odd_plan(plan, T, k, gone)
+    x, w, dy = _randn(gen, T, K, dtype=dtype), _randn(gen, E, N, K, dtype=dtype), _randn(gen, T * k, N, dtype=dtype)
+    x[0] = 1.0
+    got, whole = (g.expert_backward(dy, x, w, p, relu_input=True, need_dw=False)[0] for p in (odd, plan))
+    assert (got[gone] == 0).all() and torch.equal(got[keep], whole[keep])
+    got, whole = (g.expert_backward(dy, x, w, p, need_dw=False)[0] for p in (odd, plan))
+    assert torch.equal(got, whole)                   # without it, dx does not read x
