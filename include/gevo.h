@@ -536,9 +536,12 @@ void gevo_cnn_destroy(gevo_cnn* h);
  * several streams.  Arguments are checked before any HIP call: GEVO_E_ARG for
  * a null or misaligned pointer (of its element's size, 16 bytes for 4-bit
  * codes and 4 for their scales) or a bad enum, GEVO_E_SHAPE for a size of 0
- * or a stride below a row, GEVO_E_UNSUPPORTED beyond the limits.  No rows (T
- * or S of 0) is allowed: outputs over rows are then left, sums are 0.  Strides
- * count elements.  Results are the same bits on every run.
+ * or a stride below a row, GEVO_E_UNSUPPORTED beyond the limits, which products
+ * have one more of: R rows over E matrices to outputs of C columns have (R / 256
+ * + min(R, E)) ceil(C / 256) below 2^23 (a gradient of weights: E ceil(N / 256)
+ * ceil(K / 256)).  No rows (T or S of 0) is allowed: outputs over rows are then
+ * left, sums are 0.  Strides count elements.  Results are the same bits on every
+ * run.
  *
  * Sums, softmax, scores and joins are held in fp32; an output in bf16 is
  * rounded once, to nearest even.

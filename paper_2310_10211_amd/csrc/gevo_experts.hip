@@ -1067,8 +1067,15 @@ ExpertArgs with_divisor(ExpertArgs a) {
   return a;
 }
 
+// whether a launch, which counts its work-items in 32 bits, holds so many tiles
+template <typename SH>
+bool tiles_fit(int64_t tiles) {
+  return (tiles + 7) / 8 * 8 * SH::kThreads <= 0xffffffffll;
+}
+
 template <typename SH, ExpertType TY, Pass PASS, Load XL, Load WL, bool OUT16>
 hipError_t tile_go(const ExpertArgs& a, int64_t tiles, hipStream_t s) {
+  if (!tiles_fit<SH>(tiles)) return hipErrorInvalidValue;
   constexpr size_t lds =
       2 * (size_t)(SH::kXBytes + SH::kWBytes + (TY == kTypeMx4 ? SH::kScaleBytes : 0)) + SH::kWR * 4;
   static_assert(lds * SH::WGS <= 160 * 1024, "workgroups of a CU share its LDS");
@@ -1078,7 +1085,6 @@ hipError_t tile_go(const ExpertArgs& a, int64_t tiles, hipStream_t s) {
                                                hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
     if (err != hipSuccess) return err;
   }
-  if (tiles > 0x7ffffff8) return hipErrorInvalidValue;
   fn<<<(unsigned)((tiles + 7) / 8 * 8), SH::kThreads, lds, s>>>(a);
   return hipGetLastError();
 }
@@ -1095,10 +1101,11 @@ int64_t most_tiles(const ExpertArgs& a, Pass pass) {
 // Time of the tiles on 256 CUs in units of a 64 x 64 tile's share of a busy CU:
 // rounds of tiles times what a tile takes, `cost` for each 64 x 64 of it, and
 // no less than `least` for a round.  Expected tiles count half a part tile for
-// each expert with rows.
+// each expert with rows.  More tiles than a launch holds take forever.
 template <typename SH>
 int64_t tile_time(const ExpertArgs& a, Pass pass, int cost, int least) {
   int64_t n = most_tiles<SH>(a, pass);
+  if (!tiles_fit<SH>(n)) return INT64_MAX;
   if (pass != kDw && a.offsets) n -= (a.S < a.E ? a.S : a.E) * ((a.N + SH::kWR - 1) / SH::kWR) / 2;
   const int64_t area = SH::kXR / 64 * (SH::kWR / 64), t = (n + 255) / 256 * area * cost;
   return t > least * area ? t : least * area;

@@ -157,12 +157,20 @@ dim3 mx4_grid(const Mx4Args& a) {
 }
 }  // namespace
 
-template <typename S> hipError_t launch_mx4_quantize(const Mx4Args& a, hipStream_t s) {
-  if ((a.rows + 3) / 4 > 0x7fffffff) return hipErrorInvalidValue;
+template <typename S> hipError_t launch_mx4_quantize(const Mx4Args& args, hipStream_t s) {
+  Mx4Args a = args;
   const bool vec = (uintptr_t)a.x % 16 == 0 && a.stride * sizeof(S) % 16 == 0;
-  if (vec) k_mx4_quantize<S, true><<<mx4_grid(a), 256, 0, s>>>(a);
-  else k_mx4_quantize<S, false><<<mx4_grid(a), 256, 0, s>>>(a);
-  return hipGetLastError();
+  for (int64_t r = 0; r < args.rows; r += kLaunchBlocks * 4) {
+    a.rows = args.rows - r < kLaunchBlocks * 4 ? args.rows - r : kLaunchBlocks * 4;
+    a.x = (const S*)args.x + r * a.stride;
+    a.codes = args.codes + r * (a.Kp / 2);
+    a.scales = args.scales + r * (a.Kp / 32);
+    if (vec) k_mx4_quantize<S, true><<<mx4_grid(a), 256, 0, s>>>(a);
+    else k_mx4_quantize<S, false><<<mx4_grid(a), 256, 0, s>>>(a);
+    const hipError_t err = hipGetLastError();
+    if (err != hipSuccess) return err;
+  }
+  return hipSuccess;
 }
 template <typename S> hipError_t launch_mx4_dequantize(const Mx4Args& a, hipStream_t s) {
   const bool vec = (uintptr_t)a.x % 16 == 0 && a.stride * sizeof(S) % 16 == 0;

@@ -11,6 +11,9 @@ constexpr int kRouteMaxE = 2048;      // experts a row is routed over
 constexpr int kRouteMaxK = 64;        // of them chosen for a row
 constexpr int kRouteMaxGroups = 64;
 constexpr int kPlanChunk = 1024;      // slots a workgroup of the plan kernels sorts
+// A launch counts its work-items in 32 bits and drops the rest without an error:
+// rows past this many workgroups of 256 go out in further launches.
+constexpr int64_t kLaunchBlocks = 1 << 23;
 
 struct RouteArgs {
   const void* logits; int64_t stride;  // [T] rows, elements apart
@@ -38,6 +41,7 @@ struct CombineArgs {
   const float* weights;                    // [T][k] (nullable: ones)
   const int32_t* pos;                      // [T][k]
   void* y; int64_t y_stride;               // combine: out; backward: the gradient dy
+  int64_t slot0;                           // set by the launcher: backward: the launch's first slot
   void* drows; float* dweights;            // backward (either nullable)
 };
 template <typename S, typename O> hipError_t launch_combine(const CombineArgs& a, hipStream_t s);

@@ -475,15 +475,27 @@ hipError_t route_go(const RouteArgs& args, hipStream_t s) {
   constexpr int rows = 256 / L, align = NE * sizeof(S) < 16 ? NE * sizeof(S) : 16;
   RouteArgs a = args;
   a.vec = a.E == L * NE && (uintptr_t)a.logits % align == 0 && a.stride * (int64_t)sizeof(S) % align == 0;
-  const unsigned grid = (unsigned)((a.T + rows - 1) / rows);
-  if (BWD) k_route_bwd<S, L, NE><<<grid, 256, (size_t)rows * L * NE * 4, s>>>(a);
-  else k_route<S, L, NE><<<grid, 256, route_lds(a, rows, L, NE), s>>>(a);
-  return hipGetLastError();
+  for (int64_t t = 0; t < args.T; t += kLaunchBlocks * rows) {
+    a.T = args.T - t < kLaunchBlocks * rows ? args.T - t : kLaunchBlocks * rows;
+    a.logits = (const S*)args.logits + t * a.stride;
+    a.ids = args.ids + t * a.k;
+    const unsigned grid = (unsigned)((a.T + rows - 1) / rows);
+    if (BWD) {
+      a.dweights = args.dweights + t * a.k;
+      a.dlogits = (S*)args.dlogits + t * a.E;
+      k_route_bwd<S, L, NE><<<grid, 256, (size_t)rows * L * NE * 4, s>>>(a);
+    } else {
+      a.weights = args.weights + t * a.k;
+      k_route<S, L, NE><<<grid, 256, route_lds(a, rows, L, NE), s>>>(a);
+    }
+    const hipError_t err = hipGetLastError();
+    if (err != hipSuccess) return err;
+  }
+  return hipSuccess;
 }
 
 template <typename S, bool BWD>
 hipError_t route_shape(const RouteArgs& a, hipStream_t s) {
-  if (a.T > (int64_t)4 * 0x7fffffff) return hipErrorInvalidValue;
   if (a.E > kRouteMaxE || a.k > kRouteMaxK || a.groups > kRouteMaxGroups) return hipErrorInvalidValue;
   if (a.E <= 256 && a.k <= 16 && a.groups <= 16) {
     if (a.E <= 64) return route_go<S, BWD, 16, 4>(a, s);
@@ -721,11 +733,11 @@ __device__ __forceinline__ void store_f(S* p, int valid, const float (&f)[V]) {
 // y[t] = sum_j w[t][j] rows[pos[t][j]], summed in j's order in 32 bits and
 // rounded once; a slot without a row adds w 0.  A thread takes V columns of a row t.
 template <typename S, typename O, int V, bool WHOLE>
-__global__ __launch_bounds__(256) void k_combine(CombineArgs a, int cols, int64_t total) {
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+__global__ __launch_bounds__(256) void k_combine(CombineArgs a, uint32_t cols, uint32_t total) {
+  const uint32_t i = blockIdx.x * 256 + threadIdx.x;
   if (i >= total) return;
-  const int64_t t = total <= 0xffffffffll ? (int64_t)((uint32_t)i / (uint32_t)cols) : i / cols;
-  const int c = (int)(i - t * cols) * V;
+  const int64_t t = i / cols;
+  const int c = (int)(i - (uint32_t)t * cols) * V;
   float acc[V];
 #pragma unroll
   for (int v = 0; v < V; ++v) acc[v] = 0.0f;
@@ -753,7 +765,7 @@ __global__ __launch_bounds__(256) void k_combine(CombineArgs a, int cols, int64_
 template <typename S, int V, bool WHOLE>
 __global__ __launch_bounds__(256) void k_combine_bwd(CombineArgs a) {
   const int lane = threadIdx.x & 63;
-  const int64_t slot = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  const int64_t slot = a.slot0 + (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
   if (slot >= a.T * a.k) return;
   const int64_t t = slot / a.k;
   const int32_t p = (uint32_t)a.pos[slot] < (uint32_t)a.S ? a.pos[slot] : -1;
@@ -791,14 +803,23 @@ bool vec_ok(const void* p, int64_t stride, int N, int V, size_t elt) {
 }  // namespace
 
 template <typename S, typename O>
-hipError_t launch_combine(const CombineArgs& a, hipStream_t s) {
+hipError_t launch_combine(const CombineArgs& args, hipStream_t s) {
+  CombineArgs a = args;
   const bool whole = vec_ok(a.rows, a.rows_stride, a.N, 4, sizeof(S)) && vec_ok(a.y, a.y_stride, a.N, 4, sizeof(O));
-  const int cols = (a.N + 3) / 4;
-  const int64_t total = a.T * cols, grid = (total + 255) / 256;
-  if (grid > 0x7fffffff) return hipErrorInvalidValue;
-  if (whole) k_combine<S, O, 4, true><<<(unsigned)grid, 256, 0, s>>>(a, cols, total);
-  else k_combine<S, O, 4, false><<<(unsigned)grid, 256, 0, s>>>(a, cols, total);
-  return hipGetLastError();
+  const uint32_t cols = (uint32_t)(a.N + 3) / 4;
+  const int64_t most = kLaunchBlocks * 256 / cols;   // rows of a launch
+  for (int64_t t = 0; t < args.T; t += most) {
+    a.T = args.T - t < most ? args.T - t : most;
+    a.pos = args.pos + t * a.k;
+    a.weights = args.weights ? args.weights + t * a.k : nullptr;
+    a.y = (O*)args.y + t * a.y_stride;
+    const uint32_t total = (uint32_t)(a.T * cols), grid = (total + 255) / 256;
+    if (whole) k_combine<S, O, 4, true><<<grid, 256, 0, s>>>(a, cols, total);
+    else k_combine<S, O, 4, false><<<grid, 256, 0, s>>>(a, cols, total);
+    const hipError_t err = hipGetLastError();
+    if (err != hipSuccess) return err;
+  }
+  return hipSuccess;
 }
 template hipError_t launch_combine<float, float>(const CombineArgs&, hipStream_t);
 template hipError_t launch_combine<float, uint16_t>(const CombineArgs&, hipStream_t);
@@ -806,16 +827,22 @@ template hipError_t launch_combine<uint16_t, float>(const CombineArgs&, hipStrea
 template hipError_t launch_combine<uint16_t, uint16_t>(const CombineArgs&, hipStream_t);
 
 template <typename S>
-hipError_t launch_combine_backward(const CombineArgs& a, hipStream_t s) {
+hipError_t launch_combine_backward(const CombineArgs& args, hipStream_t s) {
   constexpr int V = 16 / sizeof(S);
-  const int64_t grid = (a.T * a.k + 3) / 4;
-  if (grid > 0x7fffffff) return hipErrorInvalidValue;
+  CombineArgs a = args;
   const bool vec = vec_ok(a.y, a.y_stride, a.N, V, sizeof(S)) &&
                    (!a.dweights || vec_ok(a.rows, a.rows_stride, a.N, V, sizeof(S))) &&
                    (!a.drows || vec_ok(a.drows, a.N, a.N, V, sizeof(S)));
-  if (vec) k_combine_bwd<S, V, true><<<(unsigned)grid, 256, 0, s>>>(a);
-  else k_combine_bwd<S, V, false><<<(unsigned)grid, 256, 0, s>>>(a);
-  return hipGetLastError();
+  const int64_t slots = a.T * a.k;
+  for (a.slot0 = 0; a.slot0 < slots; a.slot0 += kLaunchBlocks * 4) {
+    const int64_t left = slots - a.slot0;
+    const unsigned grid = (unsigned)(left < kLaunchBlocks * 4 ? (left + 3) / 4 : kLaunchBlocks);
+    if (vec) k_combine_bwd<S, V, true><<<grid, 256, 0, s>>>(a);
+    else k_combine_bwd<S, V, false><<<grid, 256, 0, s>>>(a);
+    const hipError_t err = hipGetLastError();
+    if (err != hipSuccess) return err;
+  }
+  return hipSuccess;
 }
 template hipError_t launch_combine_backward<float>(const CombineArgs&, hipStream_t);
 template hipError_t launch_combine_backward<uint16_t>(const CombineArgs&, hipStream_t);

@@ -790,3 +790,104 @@ def test_a_row_outside_x_clears_its_gradient(dtype, K, T):
     assert (got[gone] == 0).all() and torch.equal(got[keep], whole[keep])
     got, whole = (g.expert_backward(dy, x, w, p, need_dw=False)[0] for p in (odd, plan))
     assert torch.equal(got, whole)                   # without it, dx does not read x
+
+
+# A launch holds fewer than 2^32 work-items: rows past what one holds go out in several.
+def _pieces(n, at=1 << 24):
+    return [slice(r, min(n, r + at)) for r in range(0, n, at)]
+
+
+def test_more_rows_than_a_launch_holds_route():
+    T, E, k = (1 << 26) + 77, 17, 17                 # 64 lanes a row
+    logits = torch.empty(T, E, dtype=torch.bfloat16, device="cuda").normal_(generator=_rng("launch"))
+    w, ids = g.route(logits, k)
+    for p in _pieces(T):
+        a, b = g.route(logits[p], k)
+        assert torch.equal(a, w[p]) and torch.equal(b, ids[p])
+    got = g.route_backward(logits, ids, w)
+    for p in _pieces(T):
+        assert torch.equal(g.route_backward(logits[p], ids[p], w[p]), got[p])
+    del logits, w, ids, got, a, b
+    torch.cuda.empty_cache()
+
+
+def test_more_rows_than_a_launch_holds_quantize():
+    rows, K = (1 << 26) + 77, 3
+    x = torch.empty(rows, K, dtype=torch.bfloat16, device="cuda").normal_(generator=_rng("launch", 2))
+    q = g.mx4_quantize(x)
+    y = q.dequantize(torch.bfloat16)
+    for p in _pieces(rows):
+        s = g.mx4_quantize(x[p])
+        assert torch.equal(s.codes, q.codes[p]) and torch.equal(s.scales, q.scales[p])
+        assert torch.equal(s.dequantize(torch.bfloat16), y[p])
+    del x, q, y, s
+    torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("T,k", [((1 << 24) + 19, 5), (1, (1 << 26) + 77)])
+def test_more_rows_than_a_launch_holds_join_gradient(T, k):
+    gen = _rng("launch", 3)
+    n = T * k
+    pos = (torch.arange(n, dtype=torch.int32, device="cuda") ^ 5).clamp(max=n - 1)
+    pos[n - 8:] = torch.arange(n - 8, n, dtype=torch.int32, device="cuda")       # (a permutation up to its end)
+    lone = torch.arange(n, device="cuda") ^ 5
+    pos[(lone >= n - 8) & (torch.arange(n, device="cuda") < n - 8)] = -1
+    pos[::1001] = -1
+    plan = g.RoutePlan(torch.zeros(n, dtype=torch.int32, device="cuda"), pos.view(T, k),
+                       torch.tensor([0, n], dtype=torch.int32, device="cuda"))
+    rows = torch.randn(n, 2, generator=gen, device="cuda")
+    wt, dy = torch.rand(T, k, generator=gen, device="cuda"), torch.randn(T, 2, generator=gen, device="cuda")
+    drows, dw = g.expert_combine_backward(dy, rows, plan, wt)
+    have = pos >= 0
+    at = pos.clamp(min=0).long()
+    d = dy.repeat_interleave(k, 0)
+    r = rows[at]
+    want = torch.where(have, d[:, 0] * r[:, 0] + d[:, 1] * r[:, 1], 0.0)
+    mag = (d * r).abs().sum(1)
+    assert ((dw.view(-1) - want).abs() <= 8 * 2.0 ** -24 * mag).all()        # two products and a sum, rounded or fused
+    assert torch.equal(drows[at[have]], (wt.view(-1, 1) * d)[have])
+    del rows, drows, dw, d, r, want, mag, at, have, lone
+    torch.cuda.empty_cache()
+
+
+def test_more_columns_than_a_launch_holds_join():
+    """2^34 and some outputs: rows of 2^20, most of whose slots have no row."""
+    import ctypes
+    from paper_2310_10211_amd import operators as o
+    T, k, N, R = (1 << 14) + 3, 2, 1 << 20, 4
+    rows = torch.randn(R, N, generator=_rng("launch", 4), device="cuda").bfloat16()
+    pos = torch.full((T, k), -1, dtype=torch.int32, device="cuda")
+    some = {0: (0, 1), 8191: (2, -1), 8192: (-1, 3), 16383: (1, 2), T - 1: (3, 0)}
+    for t, p in some.items():
+        pos[t] = torch.tensor(p, dtype=torch.int32, device="cuda")
+    y = torch.full((T, N), 7.0, dtype=torch.bfloat16, device="cuda")
+    cfg = o.CombineConfig(1, 1, 1, k, N, T, N, N)
+    assert g.lib().gevo_expert_combine(ctypes.byref(cfg), rows.data_ptr(), pos.data_ptr(), None, y.data_ptr(),
+                                       torch.cuda.current_stream().cuda_stream) == 0
+    for t in range(0, T, 1024):
+        piece = y[t:t + 1024]
+        here = torch.zeros(len(piece), dtype=torch.bool, device="cuda")
+        for s, p in some.items():
+            if t <= s < t + len(piece):
+                here[s - t] = True
+                want = sum((rows[i].float() for i in p if i >= 0), torch.zeros(N, device="cuda")).bfloat16()
+                assert torch.equal(y[s], want)
+        assert (piece[~here] == 0).all()
+    del y, rows
+    torch.cuda.empty_cache()
+
+
+def test_more_small_tiles_than_a_launch_holds():
+    """One expert of one weight on 2^30 and some slots: tiles of 64 rows would be more work-items than a launch takes."""
+    T, k = 1025, 1 << 20
+    ids = torch.zeros(T, k, dtype=torch.int32, device="cuda")
+    plan = g.route_plan(ids, 1)
+    del ids
+    x = torch.randn(T, 1, generator=_rng("launch", 5), device="cuda").bfloat16()
+    w = torch.full((1, 1, 1), 0.5, dtype=torch.bfloat16, device="cuda")
+    y = g.expert_forward(x, w, plan)
+    assert torch.equal(y.view(T, k), (x * 0.5).expand(T, k))
+    dx = g.expert_backward(y, x, w, plan, need_dw=False)[0]
+    assert torch.equal(dx.view(T, k), (x * 0.25).expand(T, k))
+    del plan, x, w, y, dx
+    torch.cuda.empty_cache()

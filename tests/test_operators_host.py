@@ -224,6 +224,26 @@ def test_what_is_no_number_is_refused():
             o._out_dtype(bad, torch.float32)
 
 
+def test_products_of_more_tiles_than_a_launch_holds():
+    """Refused on the host: a launch would drop the tiles past 2^32 work-items."""
+    from paper_2310_10211_amd import operators as o
+    L = _lib()
+    top, wide = (1 << 31) - 1, 1 << 20
+    for over in (dict(T=top, k=1, E=1, N=1, K=1, x_stride=1, w_stride_n=1, y_stride=1),
+                 dict(T=1 << 24, k=1, N=wide, K=1, x_stride=1, w_stride_n=1, w_stride_e=wide, y_stride=wide)):
+        for dtype in (0, 1):
+            c = _fill(o.ExpertConfig, EXPERT, dict(over, dtype=dtype))
+            assert L.gevo_expert_forward(c, P, P, None, P, P, P, None) == E_UNSUPPORTED
+    c = _fill(o.ExpertConfig, EXPERT, dict(T=1 << 24, k=1, N=1, K=wide, x_stride=wide, w_stride_n=wide, w_stride_e=wide,
+                                           y_stride=1))
+    assert L.gevo_expert_backward(c, P, P, P, P, P, P, None, None, None) == E_UNSUPPORTED
+    c = _fill(o.ExpertConfig, EXPERT, dict(E=2048, T=5, N=wide, K=wide, x_stride=wide, w_stride_n=wide,
+                                           w_stride_e=1 << 40, y_stride=wide))
+    assert L.gevo_expert_backward(c, P, P, P, P, P, None, P, P, None) == E_UNSUPPORTED
+    for over in (dict(P=1, M=top, N=1), dict(P=1, M=1 << 24, N=wide)):
+        assert L.gevo_mx4_matmul(_fill(o.Mx4Config, MX4, over), P, P, P, P, None, None, None, P, None) == E_UNSUPPORTED
+
+
 # ------------------------------------------------------------- the oracle itself
 def test_oracle_route_closed_forms():
     l = [math.log(4), math.log(1), math.log(3), -math.inf]
