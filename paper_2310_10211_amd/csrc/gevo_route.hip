@@ -475,6 +475,14 @@ hipError_t route_go(const RouteArgs& args, hipStream_t s) {
   constexpr int rows = 256 / L, align = NE * sizeof(S) < 16 ? NE * sizeof(S) : 16;
   RouteArgs a = args;
   a.vec = a.E == L * NE && (uintptr_t)a.logits % align == 0 && a.stride * (int64_t)sizeof(S) % align == 0;
+  const size_t lds = BWD ? (size_t)rows * L * NE * 4 : route_lds(a, rows, L, NE);
+  if constexpr (!BWD && NE == 32) {                  // 64 KB for groups, beside the choices' 1 KB
+    if (lds > 0) {
+      const hipError_t err = hipFuncSetAttribute(reinterpret_cast<const void*>(k_route<S, L, NE>),
+                                                 hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+      if (err != hipSuccess) return err;
+    }
+  }
   for (int64_t t = 0; t < args.T; t += kLaunchBlocks * rows) {
     a.T = args.T - t < kLaunchBlocks * rows ? args.T - t : kLaunchBlocks * rows;
     a.logits = (const S*)args.logits + t * a.stride;
@@ -483,10 +491,10 @@ hipError_t route_go(const RouteArgs& args, hipStream_t s) {
     if (BWD) {
       a.dweights = args.dweights + t * a.k;
       a.dlogits = (S*)args.dlogits + t * a.E;
-      k_route_bwd<S, L, NE><<<grid, 256, (size_t)rows * L * NE * 4, s>>>(a);
+      k_route_bwd<S, L, NE><<<grid, 256, lds, s>>>(a);
     } else {
       a.weights = args.weights + t * a.k;
-      k_route<S, L, NE><<<grid, 256, route_lds(a, rows, L, NE), s>>>(a);
+      k_route<S, L, NE><<<grid, 256, lds, s>>>(a);
     }
     const hipError_t err = hipGetLastError();
     if (err != hipSuccess) return err;

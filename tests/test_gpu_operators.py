@@ -891,3 +891,42 @@ def test_more_small_tiles_than_a_launch_holds():
     assert torch.equal(dx.view(T, k), (x * 0.25).expand(T, k))
     del plan, x, w, y, dx
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("E,k,groups", [(2000, 6, 8), (1030, 3, 2), (1500, 64, 60), (2048, 9, 64), (1100, 5, 55)])
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+def test_route_over_many_experts_in_groups_of_any_size(E, k, groups, score):
+    """Past 1,024 experts, groups that are a power of two of whole lanes and ones that
+    pass through memory on chip, with keys that 32 bits order and that they do not."""
+    print(f"[gpu] route {E} {k} {groups} {score}", flush=True)
+    gen = _rng("many", E, groups)
+    top = max(1, groups // 2)
+    wide = _randn(gen, 9, E, by=2.0)
+    wide[:, ::5] = float("-inf")
+    bias = _randn(gen, E, by=0.2)
+    _check_route(wide, k, dict(score=score, groups=groups, top_groups=top))
+    _check_route(wide.bfloat16(), k, dict(score=score, groups=groups, top_groups=top, group_top=2, renorm=False))
+    _check_route(wide, k, dict(score=score, groups=groups, top_groups=top, group_top=2, bias=bias, scale=2.5))
+    l = _randn(gen, 3, E)
+    for t in range(3):                               # key = s + bias = 0.5 to the bias's rounding
+        near = torch.tensor((0.5 - ref.scores(_np(l[t]), score)).astype(np.float32), device="cuda")
+        _check_route(l[t:t + 1], k, dict(score=score, groups=groups, top_groups=top, group_top=2, bias=near))
+
+
+def test_route_over_many_experts_captured_and_replayed():
+    gen = _rng("many graph")
+    logits, bias = _randn(gen, 40, 2000), _randn(gen, 2000, by=0.2)
+    run = lambda: g.route(logits, 6, bias=bias, groups=8, top_groups=3, group_top=2)    # noqa: E731
+    run()
+    torch.cuda.synchronize()
+    stream, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        outs = run()
+    for i in range(3):
+        logits.copy_(_randn(gen, 40, 2000))
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(outs, run()):
+            assert torch.equal(a, b), i
+        torch.cuda.synchronize()
