@@ -425,18 +425,24 @@ class Population:
     def layer_weights(self, layer: int, dtype=None):
         """(w [P][d_l][d_{l-1}], b [P][d_l] float32) of layer 1 .. L of every
         variant, as device tensors (gevo_pop_layer_weights); dtype torch.float32
-        or torch.bfloat16, by default the population's."""
+        or torch.bfloat16, by default the population's.  The population's stream
+        writes them and torch's current stream waits for that."""
         torch = self.torch
         if dtype is None:
             dtype = torch.bfloat16 if self._cfg.dtype == BF16 else torch.float32
         if not 1 <= layer < len(self.dims) or dtype not in (torch.float32, torch.bfloat16):
             raise GevoError(f"layer_weights: layer {layer} of {len(self.dims) - 1}, {dtype}")
         K, N = self.dims[layer - 1], self.dims[layer]
+        current = torch.cuda.current_stream(self.workspace.device)
         with torch.cuda.stream(self.stream):
             w = torch.empty((self.P, N, K), dtype=dtype, device=self.workspace.device)
             b = torch.empty((self.P, N), dtype=torch.float32, device=self.workspace.device)
         _check(lib().gevo_pop_layer_weights(self._h, layer, BF16 if dtype == torch.bfloat16 else F32, w.data_ptr(),
                                             b.data_ptr()), "gevo_pop_layer_weights")
+        if current != self.stream:
+            current.wait_stream(self.stream)
+            w.record_stream(current)
+            b.record_stream(current)
         return w, b
 
     def predict_mx4(self) -> dict:

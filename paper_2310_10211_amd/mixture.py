@@ -36,13 +36,9 @@ class Mixture:
         self.numerics = numerics or ("bf16" if pop._cfg.dtype == BF16 else "f32")
         self.dtype = torch.bfloat16 if self.numerics == "bf16" else torch.float32
         self.dims = list(pop.dims)
-        current = torch.cuda.current_stream(pop.workspace.device)
         self.layers = []
         for l in range(1, len(self.dims)):
             w, b = pop.layer_weights(l, self.dtype)
-            current.wait_stream(pop.stream)          # which writes them
-            w.record_stream(current)
-            b.record_stream(current)
             if variants is not None:
                 index = torch.as_tensor(variants, device=w.device, dtype=torch.long)
                 if index.dim() != 1 or index.numel() == 0 or int(index.min()) < 0 or int(index.max()) >= pop.P:

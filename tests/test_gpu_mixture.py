@@ -216,3 +216,25 @@ def test_the_gates_gradient_takes_the_predictions_scale():
     want = Mixture.gate_gradient(m.predict(x, gate, 2, scale=1.5)[1], dl)
     assert torch.equal(Mixture.gate_gradient(state, dl), want)
     pop.close()
+
+
+def test_layer_weights_are_there_for_the_current_stream():
+    """Read at once on another stream than the population's, behind work that it still has to do."""
+    stream = torch.cuda.Stream()
+    with torch.cuda.stream(stream):
+        pop = _population([784, 128, 10], 16, "bf16", n_train=4000, epochs=3, stream=stream)
+    got = [[t.clone() for t in pop.layer_weights(l, torch.float32)] for l in (1, 2)]
+    torch.cuda.synchronize()
+    for l in (1, 2):
+        assert all(torch.equal(a, b) for a, b in zip(got[l - 1], pop.layer_weights(l, torch.float32)))
+    before = pop.layer_weights(1, torch.float32)[0]
+    other = torch.cuda.Stream()
+    with torch.cuda.stream(other):                   # memory given back while another stream reads it is not handed out
+        w = pop.layer_weights(1, torch.float32)[0]
+        copy = w.clone()
+        del w
+    with torch.cuda.stream(stream):
+        torch.full_like(before, 7.0)
+    torch.cuda.synchronize()
+    assert torch.equal(copy, before)
+    pop.close()
