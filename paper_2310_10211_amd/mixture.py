@@ -111,10 +111,12 @@ class Mixture:
 def scores(logits, labels):
     """(mean cross-entropy, accuracy) of logits [..., rows][classes] against labels
     [rows]: argmax with the lowest index on ties, a NaN logit a miss and its
-    loss NaN, as Population.scores counts them."""
+    loss NaN, as Population.scores counts them; so is a label that is no class."""
     labels = labels.long().expand(logits.shape[:-1])
-    loss = torch.logsumexp(logits, -1) - logits.gather(-1, labels[..., None])[..., 0]
+    known = (labels >= 0) & (labels < logits.shape[-1])
+    own = logits.gather(-1, torch.where(known, labels, 0)[..., None])[..., 0]
+    loss = torch.where(known, torch.logsumexp(logits, -1) - own, torch.nan)
     top = logits.amax(-1, keepdim=True)
     index = torch.arange(logits.shape[-1], device=logits.device)
     first = torch.where(logits == top, index, logits.shape[-1]).amin(-1)
-    return loss.mean(-1), (first == labels).float().mean(-1)
+    return loss.mean(-1), (known & (first == labels)).float().mean(-1)

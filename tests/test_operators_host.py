@@ -244,6 +244,20 @@ def test_products_of_more_tiles_than_a_launch_holds():
         assert L.gevo_mx4_matmul(_fill(o.Mx4Config, MX4, over), P, P, P, P, None, None, None, P, None) == E_UNSUPPORTED
 
 
+def test_scores_of_labels_that_are_no_class():
+    """A label outside the classes reads no logit: its loss is NaN, and it is a miss."""
+    import torch
+    from paper_2310_10211_amd.mixture import scores
+    nan = math.nan
+    logits = torch.tensor([[[1.0, 2.0, 0.0], [0.0, 2.0, 2.0]], [[1.0, 2.0, 0.0], [nan, 0.0, 1.0]]])
+    for bad in (-1, 3, -(1 << 31), (1 << 31) - 1):
+        loss, acc = scores(logits, torch.tensor([1, bad], dtype=torch.int32))
+        assert loss.isnan().all() and acc.tolist() == [0.5, 0.5]
+    loss, acc = scores(logits[:1], torch.tensor([1, 2]))
+    want = (math.log(1 + math.exp(-1) + math.exp(-2)) + math.log(2 + math.exp(-2))) / 2
+    assert abs(float(loss[0]) - want) < 1e-6 and acc.tolist() == [0.5]
+
+
 # ------------------------------------------------------------- the oracle itself
 def test_oracle_route_closed_forms():
     l = [math.log(4), math.log(1), math.log(3), -math.inf]
