@@ -26,6 +26,18 @@ from .operators import (_number, expert_combine, expert_combine_backward, expert
                         route, route_backward, route_plan)
 
 
+def _indices(variants, n, device):
+    """variants as a tensor of indices below n; neither masks nor fractions are any."""
+    try:
+        index = torch.as_tensor(variants)
+    except (TypeError, ValueError, RuntimeError):
+        index = torch.empty(0)
+    if (index.dim() != 1 or index.numel() == 0 or index.dtype == torch.bool or index.is_floating_point() or
+            index.is_complex() or int(index.min()) < 0 or int(index.max()) >= n):
+        raise GevoError(f"variants: indices in [0, {n})")
+    return index.to(device, torch.long)
+
+
 class Mixture:
     """Copies of the layers of a population's variants (all, or `variants`), in
     numerics "f32", "bf16" or "mx4" (None: the population's own type)."""
@@ -37,12 +49,10 @@ class Mixture:
         self.dtype = torch.bfloat16 if self.numerics == "bf16" else torch.float32
         self.dims = list(pop.dims)
         self.layers = []
+        index = None if variants is None else _indices(variants, pop.P, pop.workspace.device)
         for l in range(1, len(self.dims)):
             w, b = pop.layer_weights(l, self.dtype)
-            if variants is not None:
-                index = torch.as_tensor(variants, device=w.device, dtype=torch.long)
-                if index.dim() != 1 or index.numel() == 0 or int(index.min()) < 0 or int(index.max()) >= pop.P:
-                    raise GevoError(f"variants: indices in [0, {pop.P})")
+            if index is not None:
                 w, b = w[index], b[index]
             self.layers.append((mx4_quantize(w) if self.numerics == "mx4" else w, b))
         self.n_variants = self.layers[0][1].shape[0]

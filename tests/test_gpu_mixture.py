@@ -238,3 +238,14 @@ def test_layer_weights_are_there_for_the_current_stream():
     torch.cuda.synchronize()
     assert torch.equal(copy, before)
     pop.close()
+
+
+def test_variants_are_whole_indices():
+    pop = _population([40, 10], 3, "f32")
+    want = Mixture(pop, variants=[2, 0])
+    for same in ((2, 0), np.array([2, 0]), torch.tensor([2, 0]), torch.tensor([2, 0], device="cuda", dtype=torch.int32)):
+        assert torch.equal(Mixture(pop, variants=same).layers[0][0], want.layers[0][0])
+    for bad in ([True, False, True], torch.tensor([True, False, True]), [0.0, 1.9], np.array([0.5]), ["0"], 1):
+        with pytest.raises(g.GevoError):
+            Mixture(pop, variants=bad)
+    pop.close()
