@@ -175,7 +175,7 @@ __global__ __launch_bounds__(256, NE == 16 ? 6 : 1) void k_route(RouteArgs a) {
     auto more = [](K x, K y) { return x > y ? x : y; };
     auto less = [](K x, K y) { return x < y ? x : y; };
     K key[NE];
-    F tol = 0;
+    F tol = 0, group_tol = 0;                        // of two keys, of two groups' values
     if constexpr (wide) {
       load_logits();
       load_biases();
@@ -203,12 +203,20 @@ __global__ __launch_bounds__(256, NE == 16 ? 6 : 1) void k_route(RouteArgs a) {
 #pragma unroll
         for (int j = 0; j < NE; ++j) score[j] *= top;
       }
-      // What two keys in 32 bits can be off by together.  exp2's argument is
-      // rounded to |x| 2^-24 log2 e, which x s (1 - s) <= 0.23 and d e^-d <= 0.37
-      // keep below 4e-8 of a score; its result, the sum with 1 and the reciprocal
-      // add a step (1.2e-7) each at most, the sum over a row 4e-7, the sum with
-      // the bias half a step of itself; a group adds two keys.
-      if (!wide) tol = 2 * ((a.sigmoid ? 5e-7f : 1e-6f) * top + 6e-8f * (top + (F)bmax)) * a.group_top;
+      // What two keys in 32 bits can be off by together.  exp2's argument is off by
+      // 1.4e-7 of |x| at most (x, its product, log2 e), which x s (1 - s) <= 0.23
+      // and x e^-x <= 0.37 keep below 5e-8 of a score; its result, the sum with 1
+      // and the reciprocal or the product add a step (1.2e-7) each at most.  A
+      // softmax's sum carries its terms' errors, 1.4e-7 times their mean x, below
+      // ln 2048, and their step, and NE + 6 half steps of its own, in all below
+      // 1.2e-6 + 6e-8 (NE + 6), of both scores alike.  The sum with the bias is off
+      // by half a step of itself.  A group adds two keys, to half a step of twice
+      // their bound.
+      if (!wide) {
+        const F half = 6e-8f * (top + (F)bmax);
+        tol = 2 * ((a.sigmoid ? 5e-7f : 1e-6f + 3e-8f * (NE + 6)) * top + half);
+        group_tol = a.group_top == 2 ? 2 * tol + 4 * half : tol;
+      }
 #pragma unroll
       for (int j = 0; j < NE; ++j) key[j] = ordered(l[j] == ninf ? flowest : score[j] + (F)b[j]);
     }
@@ -249,7 +257,7 @@ __global__ __launch_bounds__(256, NE == 16 ? 6 : 1) void k_route(RouteArgs a) {
       for (int i = 0; i <= a.top_groups && i < a.groups; ++i) {
         const F mx = row_reduce<L>(v, [](F x, F y) { return x > y ? x : y; });
         if (i == a.top_groups) {
-          if (!(last - mx > tol) && last > flowest) sure = false;
+          if (!(last - mx > group_tol) && last > flowest) sure = false;
           break;
         }
         // lanes and groups ascend together: the first lane has the lowest group

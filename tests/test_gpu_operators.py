@@ -930,3 +930,25 @@ def test_route_over_many_experts_captured_and_replayed():
         for a, b in zip(outs, run()):
             assert torch.equal(a, b), i
         torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("E,groups", [(16, 8), (64, 8), (2000, 8)])
+def test_route_groups_whose_sums_nearly_tie(E, groups):
+    """Two groups of two keys with a bias in common, every rounding of 32 bits against
+    the larger one: key halves that go to the even step below and above, and sums that do."""
+    gen, T, gs = _rng("sums", E), 1 << 15, E // groups
+    for base in (1.0, 16.0, 64.0):
+        step = base * 2.0 ** -23
+        j = 4 * torch.randint(0, 64, (T, 1), generator=gen, device="cuda") + 1
+        r = torch.rand(T, 4, generator=gen, device="cuda", dtype=torch.float64)
+        h = 0.5 + j.double() * step / 2 + (r - 0.5) * 2e-7
+        logits, bias = torch.full((T, E), -30.0, device="cuda"), torch.zeros(E, device="cuda")
+        for c, (e, add) in enumerate(((0, 256), (1, 1), (gs, 257), (gs + 1, 0))):
+            logits[:, e] = torch.log(h / (1 - h))[:, c].float()
+            bias[e] = base + add * step
+        ids = g.route(logits, 1, score="sigmoid", bias=bias, groups=groups, top_groups=1, group_top=2)[1][:, 0].long()
+        key = torch.sigmoid(logits.double()) + bias.double()
+        sums = key[:, [0, gs]] + key[:, [1, gs + 1]]
+        apart = (sums[:, 0] - sums[:, 1]).abs() > 1e-13        # (of a binary64's own rounding)
+        assert apart.float().mean() > 0.99
+        assert torch.equal(ids[apart], torch.where(sums[:, 0] > sums[:, 1], 0, gs)[apart])
