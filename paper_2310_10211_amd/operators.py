@@ -144,8 +144,6 @@ def _u32_ok(name, value):
 # Numbers of the caller's as plain ones, read at the call: a tensor or an array
 # of one value can change, and would be kept by its identity below.
 def _index(name, value):
-    if type(value) is int:
-        return value
     try:
         return operator.index(value)
     except (TypeError, ValueError, RuntimeError):
@@ -153,12 +151,10 @@ def _index(name, value):
 
 
 def _number(name, value):
-    if type(value) is not float:
-        try:
-            value = ctypes.c_float(value).value
-        except (TypeError, ValueError, RuntimeError, OverflowError):
-            raise GevoError(f"{name}: a number, not {value!r}") from None
-    return value + 0.0                               # (-0 and 0 are one key)
+    try:
+        return ctypes.c_float(value).value + 0.0     # (-0 and 0 are one key)
+    except (TypeError, ValueError, RuntimeError, OverflowError):
+        raise GevoError(f"{name}: a number, not {value!r}") from None
 
 
 # The configurations of calls, by their values, which are plain numbers: a program
@@ -213,15 +209,17 @@ def _plan_of(plan, device):
 def _route_config(logits, k, score, groups, top_groups, group_top, renorm, scale):
     if not isinstance(score, str) or score not in SCORES:
         raise GevoError(f"score: one of {sorted(SCORES)}, not {score!r}")
-    k, groups = _index("top_k", k), _index("groups", groups)
-    top_groups, group_top = _index("top_groups", top_groups), _index("group_top", group_top)
+    if not type(k) is type(groups) is type(top_groups) is type(group_top) is int:
+        k, groups = _index("top_k", k), _index("groups", groups)
+        top_groups, group_top = _index("top_groups", top_groups), _index("group_top", group_top)
     if min(k, groups, top_groups, group_top) < 1:
         raise GevoError("top_k, groups, top_groups and group_top: at least 1")
     T, E = logits.shape
     if k > E:
         raise GevoError(f"top_k: at most the {E} experts, not {k}")
+    scale = scale + 0.0 if type(scale) is float else _number("scale", scale)
     return _route_cfg(E, k, T, DTYPES[logits.dtype], SCORES[score], _stride(logits) if T > 1 else E, groups,
-                      top_groups, group_top, 1 if renorm else 0, _number("scale", scale))
+                      top_groups, group_top, 1 if renorm else 0, scale)
 
 
 def route(logits, top_k, *, score="softmax", bias=None, groups=1, top_groups=1, group_top=1, renorm=True, scale=1.0):
@@ -233,7 +231,8 @@ def route(logits, top_k, *, score="softmax", bias=None, groups=1, top_groups=1, 
         bias = _flat(bias, "bias", torch.float32, logits.shape[1:], dev)
     if logits.shape[0] > 1 and logits.stride(0) < logits.shape[1]:
         logits = logits.contiguous()                 # rows that overlap (expanded)
-    top_k = _index("top_k", top_k)
+    if type(top_k) is not int:
+        top_k = _index("top_k", top_k)
     cfg = _route_config(logits, top_k, score, groups, top_groups, group_top, renorm, scale)
     T = logits.shape[0]
     weights, ids = _new_rows(T, top_k, torch.float32, dev), _new_rows(T, top_k, torch.int32, dev)
@@ -263,7 +262,8 @@ def route_plan(ids, n_experts) -> RoutePlan:
     """The slots of ids [T][k] sorted by expert (gevo_route_plan)."""
     if not (isinstance(ids, torch.Tensor) and ids.is_cuda and ids.dim() == 2):
         raise GevoError("ids: a tensor [T][k] on the GPU")
-    n_experts = _index("n_experts", n_experts)
+    if type(n_experts) is not int:
+        n_experts = _index("n_experts", n_experts)
     if n_experts < 1:
         raise GevoError("n_experts: at least 1")
     dev = ids.device
