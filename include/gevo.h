@@ -625,9 +625,9 @@ gevo_status gevo_route_plan(int64_t slots, uint32_t E, const int32_t* d_ids, voi
  *             dw[e][n][k] = sum_r dy[r][n] x[row(r)][k] and
  *             db[e][n] = sum_r dy[r][n] over expert e's rows (0 without any).
  * x, w, dy and dx have dtype; dw and db are fp32.  Sums are fp32.  A
- * gradient's outputs may be NULL; dw, db and dx are contiguous.  Sorted rows
- * from offsets[E] on are not written.  Offsets outside [0, S] are cut to it,
- * and a row outside x reads zeros.
+ * gradient's outputs may be NULL, but db comes with dw only; dw, db and dx are
+ * contiguous.  Sorted rows from offsets[E] on are not written.  Offsets outside
+ * [0, S] are cut to it, and a row outside x reads zeros.
  */
 typedef struct {
   uint32_t abi_version;

@@ -29,8 +29,10 @@ typedef float f32x4_t __attribute__((ext_vector_type(4)));
 // A workgroup's tile: RM x RN waves of (32 MI) x (32 NI), in steps of STEP
 // bytes of contraction, WGS workgroups on a CU.
 //   Wide   256 x 256, eight waves: per matrix clock of a step 32 bytes of
-//          operands from memory to LDS (a CU takes in about 47 of such loads)
-//          and 96 from LDS to the waves
+//          operands from memory to LDS and 96 from LDS to the waves.  The loop
+//          takes in 17 a clock without the products (one 8192 x 8192 matrix on
+//          8,192 rows in bf16): at most one step is under way, none between
+//          the wait for it and the next one's issue.
 //   Mid    128 x 128
 //   Small  64 x 64: products of few tiles, spread over more of the chip
 // Steps of 128 bytes read whole cache lines; Mid takes 64, whose buffers let
@@ -1102,6 +1104,17 @@ int64_t most_tiles(const ExpertArgs& a, Pass pass) {
 // rounds of tiles times what a tile takes, `cost` for each 64 x 64 of it, and
 // no less than `least` for a round.  Expected tiles count half a part tile for
 // each expert with rows.  More tiles than a launch holds take forever.
+//
+// Both sides of the lines, us for Wide / Mid / Small, forward unless stated:
+//   bf16  1024 x 1024 on 1,024 rows 27 / 16 / 10, 2048 x 1024 on 4,096 31 / 26 /
+//         37, 64 of 2048 x 1024 on 32,768 slots 169 / 216 / 309 (dx 179 / 209 /
+//         292, where Mid is taken), 32 of 1024 x 1024 on 8,192 dw 44 / 48 / 60
+//   4 bit 2048 x 1024 on 4,096 rows 17 / 14 / 21, 64 of 2048 x 1024 on 32,768
+//         slots 78 / 82 / 138
+//   fp32  2048 x 1024 on 2,048 rows 244 / 81 / 82, 64 of 2048 x 1024 on 16,384
+//         slots 737 / 657 / 631, dw 661 / 656 / 798
+// It misses by most where Wide's one round is half empty: 4096 x 1024 on 4,096
+// rows in bf16 38 / 50 / 63 takes Mid.
 template <typename SH>
 int64_t tile_time(const ExpertArgs& a, Pass pass, int cost, int least) {
   int64_t n = most_tiles<SH>(a, pass);
@@ -1129,7 +1142,11 @@ bool on_dwords(int64_t row_bytes, const void* p, int64_t a, int64_t b) {
   return ((uintptr_t)p | (uintptr_t)row_bytes | (uintptr_t)a | (uintptr_t)b) % 4 == 0 && row_bytes >= 16;
 }
 // The contraction is split where 16 columns a wave would leave the chip less
-// than eight waves a CU, if each of its parts is a few loads long.
+// than eight waves a CU, if each of its parts is a few loads long.  One row for
+// each expert of 1,024 columns in bf16, us split / whole: rows of 8 KB 9 / 21 (one
+// expert), 14 / 24 (8), 28 / 39 (24), 29 / 42 (32, taken whole), 111 / 127 (128);
+// of 2 KB 10 / 13 (24), 20 / 19 (64); of 1 KB 9 / 9 (16), 12 / 9 (24, taken split),
+// 23 / 12 (64); of 512 bytes 9 / 9 (16), 11 / 9 (24).
 template <ExpertType TY, bool OUT16>
 hipError_t few_go(const ExpertArgs& a, int64_t segs, hipStream_t s) {
   const int64_t bands = (a.N + 15) / 16;
@@ -1146,7 +1163,16 @@ hipError_t forward_out(const ExpertArgs& a, hipStream_t s) {
   // Up to 16 rows a segment on average the weights' bytes bound the product; up
   // to 64, where tiles would leave CUs idle, reading them again for every 16 rows
   // costs less than long contractions on a few CUs (81 rows over 3 experts of
-  // 1062 x 2611 in fp32: 32 us, tiles 70).
+  // 1062 x 2611 in fp32: 32 us, tiles 70).  Both sides, us for few rows / tiles:
+  //   4 experts of 1024 x 2048    bf16 16 rows each 12 / 14, 24 12 / 14, 64 28 / 15;
+  //                               fp32 16 21 / 45, 64 50 / 46
+  //   64 experts of 2048 x 1024   bf16 4 rows each 46 / 42, 16 96 / 43, 24 128 / 45;
+  //                               fp32 4 125 / 137, 16 233 / 142; 4 bit 4 20 / 18
+  //   256 experts of 512 x 784    bf16 4 rows each 43 / 41, 16 73 / 42; 4 bit 4 18 /
+  //                               23, 16 31 / 24
+  // With many experts the line lies too high, and rows that all go to one of many
+  // pass its weights once for every 16: 1,024 on one of 64 of 2048 x 2048 in bf16
+  // 963 / 22.
   const int64_t segs = a.offsets ? (a.S < a.E ? a.S : a.E) : a.E;
   if (segs <= 65535 && (a.S <= segs * 16 || (a.S <= segs * 64 && most_tiles<typename Shapes<TY>::Small>(a, kForward) < 256))) {
     return few_go<TY, OUT16>(a, segs, s);

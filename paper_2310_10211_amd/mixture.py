@@ -98,7 +98,8 @@ class Mixture:
     def predict(self, x, gate_logits, top_k, **how):
         """(logits [rows][classes] float32, state) of each row's top_k variants by
         gate_logits [rows][variants], joined with route's weights; `how` are
-        route's options.  state is what gate_gradient asks for."""
+        route's options.  state is what gate_gradient asks for; it holds
+        gate_logits themselves, whose values have to stay until then."""
         if gate_logits.shape != (x.shape[0], self.n_variants):
             raise GevoError(f"gate_logits: shape {(x.shape[0], self.n_variants)}, not {tuple(gate_logits.shape)}")
         if "scale" in how:                           # its value now, which the gradient takes too
@@ -112,7 +113,9 @@ class Mixture:
     @staticmethod
     def gate_gradient(state, dlogits):
         """Gradient with respect to predict's gate_logits, in their type, from the
-        gradient dlogits [rows][classes] float32 of its logits."""
+        gradient dlogits [rows][classes] float32 of its logits.  autograd sees
+        none of this: gate_logits.backward(gate_gradient(state, dlogits)) carries
+        it on to a gate made of torch modules."""
         gate_logits, weights, ids, plan, rows, how = state
         _, dweights = expert_combine_backward(dlogits, rows, plan, weights)
         return route_backward(gate_logits, ids, dweights, **how)

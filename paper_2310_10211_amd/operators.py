@@ -9,6 +9,10 @@ stream, so calls can be captured into a graph.  Tensors are float32 or
 bfloat16; rows may be strided, a last dimension that is not contiguous is
 copied first.  A wrong argument raises GevoError and launches nothing.
 
+These calls are not recorded by autograd: an output does not ask for a
+gradient, whatever its inputs do.  Gradients are the calls named backward,
+whose results the caller hands on (logits.backward(route_backward(...))).
+
     weights, ids = route(logits, top_k)              # [T][k] each
     plan = route_plan(ids, n_experts)                # slots sorted by expert
     rows = expert_forward(x, w, plan, bias, relu=True)       # [T k][N], sorted

@@ -249,3 +249,20 @@ def test_variants_are_whole_indices():
         with pytest.raises(g.GevoError):
             Mixture(pop, variants=bad)
     pop.close()
+
+
+def test_outputs_ask_for_no_gradient_and_a_gate_of_modules_trains():
+    """autograd records none of the calls; the gate's gradient is handed on to torch."""
+    pop = _population([40, 10], 5, "f32")
+    m, x = Mixture(pop), pop.x_test
+    gate = torch.nn.Linear(40, 5, device="cuda")
+    logits = gate(x)
+    z, state = m.predict(x, logits, 2)
+    assert not z.requires_grad
+    dl = torch.randn(z.shape, generator=torch.Generator("cuda").manual_seed(2), device="cuda")
+    grad = Mixture.gate_gradient(state, dl)
+    logits.backward(grad)
+    # products of at most 150 terms
+    want, mag = grad.double().T @ x.double(), grad.double().abs().T @ x.double().abs()
+    assert ((gate.weight.grad.double() - want).abs() <= 152 * 2.0 ** -23 * mag).all()
+    pop.close()
